@@ -267,6 +267,69 @@ dig_status dig_gla_bwd_multi(const void *q, const void *k, const void *v, const 
                              int d_v, int chunk, unsigned direction_mask, int dtype, void *workspace,
                              size_t workspace_bytes, void *cuda_stream);
 
+/* Linear attention with a decay for each head, forward: per (batch, head), t running over the grid in `direction`,
+ *   S_t = g S_{t-1} + k_t^T v_t,   out_t = q_t S_t,   g = exp(log_decay_per_head[h]),
+ * dig_gla_fwd with one constant gate per head (constant decays as of retention layers, 1 - 2^-5 ... , or slopes 2^(-8 h / H)), without
+ * the gate tensor's bytes.  Nothing of the paper: DiG's gates depend on the token.  No scaling and no normaliser are applied.
+ *   q: [B][L][H][d_k]; k: [B][L][H_kv][d_k]; v: [B][L][H_kv][d_v]; out: [B][L][H][d_v], dense; H a multiple of H_kv, and head h reads
+ *   key/value head h / (H / H_kv).  d_k, d_v: multiples of 8, 8..128; H at most 256.  `dtype`: DIG_F32 or DIG_BF16.
+ *   strides: HOST array of the batch and token strides of q, k and v in elements (q batch, q token, k batch, ...), multiples of 16
+ *   bytes, or NULL where all three are dense; the heads of a token always stand side by side.  Slices of a fused projection
+ *   [B][L][(H + H_kv) d_k + H_kv d_v] need no copy so.
+ *   log_decay_per_head: HOST array of H finite values <= 0.
+ *   lengths: [B] tokens of each sequence, DEVICE, or NULL for L each; values outside 0..L count as the nearest of the two.  Rows of
+ *   out behind the end of a sequence are zeros, what q, k and v hold there is not used.  Row orders only (else DIG_ERR_UNSUPPORTED).
+ *   s_in: state before the first token, fp32 [B][H][d_k][d_v], NULL = 0; s_out: receives the state after the last token, or NULL.
+ * fp32 storage: fp32 FMA arithmetic.  bf16 storage: q, k and v enter the products as they are, decayed scores, states and (for out) decayed
+ * keys as bf16, sums in fp32; s_out is accurate to about 1e-5, its decayed keys enter in two bf16 parts.
+ * A NaN or an infinity in v reaches rows of the same 32 positions before it (products with zeros), never earlier ones. */
+size_t dig_decay_workspace_bytes(int B, int H, int H_kv, int grid_h, int grid_w, int d_k, int d_v, int dtype, int backward);
+dig_status dig_decay_fwd(const void *q, const void *k, const void *v, const long long *strides, const float *log_decay_per_head,
+                         const int *lengths, const float *s_in, void *out, float *s_out, int B, int H, int H_kv, int grid_h,
+                         int grid_w, int d_k, int d_v, int direction, int dtype, void *workspace, size_t workspace_bytes,
+                         void *cuda_stream);
+
+/* Reverse mode of dig_decay_fwd: gradients of <d_out, out> + <ds_out, s_out> (NULL ds_out = 0).  Nothing is saved by the forward call.
+ *   d_out: [B][L][H][d_v], dense; dq: [B][L][H][d_k]; dk: [B][L][H_kv][d_k]; dv: [B][L][H_kv][d_v], summed over the heads that share them;
+ *   ds_in: gradient with respect to s_in, or NULL.  Rows behind the end of a sequence are zeros.  The decays get no gradient. */
+dig_status dig_decay_bwd(const void *q, const void *k, const void *v, const long long *strides, const float *log_decay_per_head,
+                         const int *lengths, const void *d_out, const float *s_in, const float *ds_out, void *dq, void *dk, void *dv,
+                         float *ds_in, int B, int H, int H_kv, int grid_h, int grid_w, int d_k, int d_v, int direction, int dtype,
+                         void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/* One more token of every sequence: s_out = g s_in + k^T v, out = q s_out, in fp32 arithmetic.
+ *   q: [B][H][d_k]; k: [B][H_kv][d_k]; v: [B][H_kv][d_v]; out: [B][H][d_v]; s_in, s_out: fp32 [B][H][d_k][d_v], which may be the
+ *   same array (the state is then updated in place). */
+dig_status dig_decay_step(const void *q, const void *k, const void *v, const float *log_decay_per_head, const float *s_in, void *out,
+                          float *s_out, int B, int H, int H_kv, int d_k, int d_v, int dtype, void *cuda_stream);
+
+/* Rotary positions with several axes (height and width of a token grid, time of a video): pair i of every head's channels is turned by
+ * the angle positions[b][l][axes[i]] * freqs[i], by its negative with `inverse` (which is the gradient).
+ *   pair i: channels (2 i, 2 i + 1) where `interleaved`, else (i, i + n_pairs); channels from 2 n_pairs on stay as they are.
+ *   q: [B][L][H][d]; k: [B][L][H_k][d] or NULL; q_out, k_out: the same, dense, or the inputs themselves (in place).
+ *   strides: HOST array of the batch and token strides of q and k in elements, multiples of 16 bytes, or NULL: dense.
+ *   positions: int32 [pos_batches][L][n_axes], DEVICE, pos_batches 1 or B; any values.
+ *   freqs: HOST array of n_pairs values (radians per position); axes: HOST array of n_pairs values in 0 .. n_axes - 1.
+ *   d: a multiple of 8, 8..128; d - 2 n_pairs a multiple of 4.  `dtype`: DIG_F32 or DIG_BF16.
+ * Angles are formed in 64 bits and reduced before they are rounded. */
+dig_status dig_rope(const void *q, const void *k, const long long *strides, const int *positions, int pos_batches, int n_axes,
+                    const double *freqs, const int *axes, int n_pairs, void *q_out, void *k_out, int B, int L, int H, int H_k, int d,
+                    int interleaved, int inverse, int dtype, void *cuda_stream);
+
+/* Layer norm over rows of D values, the norm in front of a mixer block:
+ *   y = (x - mean) / sqrt(var + eps) * w + b,   biased variance.
+ *   x, y: [rows][D]; w, b: fp32 [groups][D] or NULL (1 / 0), group i serving rows i * rows / groups ... (an image's scale and shift,
+ *   groups = 1: one set for all); rows a multiple of groups; D in 1..8192; groups at most 65535.  `dtype`: DIG_F32 or DIG_BF16. */
+dig_status dig_layernorm_fwd(const void *x, const float *w, const float *b, void *y, long long rows, int groups, int D, float eps, int dtype,
+                             void *cuda_stream);
+
+/* Reverse mode of dig_layernorm_fwd: dx from dy, and where the pointer is not NULL dw and db (fp32 [groups][D]; the gradients at weight 1
+ * where w is NULL), summed over a group's rows in a fixed order.  The workspace (dig_layernorm_bwd_workspace_bytes; 0 for invalid sizes)
+ * holds partial sums and is needed only when dw or db is requested. */
+size_t dig_layernorm_bwd_workspace_bytes(long long rows, int groups, int D);
+dig_status dig_layernorm_bwd(const void *x, const void *dy, const float *w, void *dx, float *dw, float *db, long long rows, int groups, int D,
+                             float eps, int dtype, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
 /* Synchronises `cuda_stream`, then returns and clears the status recorded by device code on the
  * current device since the last query: DIG_ERR_TIMEOUT if a bounded wait inside a kernel expired,
  * else DIG_ERR_RANGE if some gates decayed faster than the tcgen05 kernels represent (see dig_gla_fwd),

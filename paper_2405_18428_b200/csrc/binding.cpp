@@ -9,6 +9,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -488,6 +489,298 @@ PyObject *dwconv_bwd(PyObject *const *a)
     return pack({dx, dw, db});
 }
 
+// ---- linear attention with a decay for each head, rotary positions, layer norm -------------------------------------
+// These run on their tensors' device and its current stream, whatever the current device is.
+void on_cuda(const Tensor &t, const char *name)
+{
+    if (!t.is_cuda()) raise(PyExc_ValueError, std::string(name) + ": need a CUDA tensor, got one on " + t.device().str());
+}
+struct On {
+    c10::cuda::CUDAGuard guard;
+    explicit On(const Tensor &t) : guard(t.device()) {}
+    void *stream() const { return c10::cuda::getCurrentCUDAStream().stream(); }
+};
+// H numbers.
+std::vector<float> numbers(PyObject *o, int64_t H, const char *name)
+{
+    PyObject *seq = PySequence_Fast(o, "need a sequence of numbers");
+    if (!seq) throw Raised{};
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq);
+    std::vector<float> v(n);
+    bool bad = false;
+    for (Py_ssize_t i = 0; i < n && !bad; ++i) {
+        const double x = PyFloat_AsDouble(PySequence_Fast_GET_ITEM(seq, i));
+        bad = x == -1.0 && PyErr_Occurred();
+        v[i] = (float)x;
+    }
+    Py_DECREF(seq);
+    if (bad) throw Raised{};
+    if (n != H) raise(PyExc_ValueError, std::string(name) + ": " + std::to_string(n) + " values for " + std::to_string(H) + " heads");
+    return v;
+}
+// A tensor [B, L, H, d] whose heads stand side by side: its pointer, and the batch and token strides.  Strides of dimensions of one
+// element say nothing.
+void *rows(const Tensor &t, ScalarType st, const char *name, const Tensor &like, long long *strides)
+{
+    on_cuda(t, name);
+    if (t.dim() != 4) raise(PyExc_ValueError, std::string(name) + ": need 4 dimensions [B, L, H, d], got shape " + text(t.sizes()));
+    if (t.scalar_type() != st) raise(PyExc_ValueError, std::string(name) + ": need a tensor of " + c10::toString(st) + ", got " + c10::toString(t.scalar_type()));
+    if (t.device() != like.device()) raise(PyExc_ValueError, std::string(name) + ": on " + t.device().str() + ", the other tensors on " + like.device().str());
+    const int64_t H = t.size(2), d = t.size(3);
+    if (t.numel() == 0) raise(PyExc_ValueError, std::string(name) + ": empty, shape " + text(t.sizes()));
+    if ((d > 1 && t.stride(3) != 1) || (H > 1 && t.stride(2) != d))
+        raise(PyExc_ValueError, std::string(name) + ": the last two dimensions have to be dense, got strides " + text(t.strides()));
+    strides[1] = t.size(1) > 1 ? t.stride(1) : H * d;
+    strides[0] = t.size(0) > 1 ? t.stride(0) : t.size(1) * strides[1];
+    const int64_t unit = st == kF32 ? 4 : 8;
+    if (strides[0] % unit || strides[1] % unit || (reinterpret_cast<uintptr_t>(t.data_ptr()) & 15))
+        raise(PyExc_ValueError, std::string(name) + ": rows have to start on 16-byte boundaries, got strides " + text(t.strides()));
+    return t.data_ptr();
+}
+
+struct Decay {
+    const Tensor &q_t;
+    int B, L, H, Hk, dk, dv, gh, gw, dtype;
+    ScalarType st;
+    long long strides[6];
+    void *q, *k, *v;
+    std::vector<float> decay;
+    Decay(PyObject *const *a, PyObject *gh_, PyObject *gw_) : q_t(tensor(a[0], "q"))
+    {
+        const Tensor &k_t = tensor(a[1], "k"), &v_t = tensor(a[2], "v");
+        dtype = dtype_of(q_t, false);
+        st = storage(dtype);
+        q = rows(q_t, st, "q", q_t, strides);
+        k = rows(k_t, st, "k", q_t, strides + 2);
+        v = rows(v_t, st, "v", q_t, strides + 4);
+        const auto n = q_t.sizes();
+        if (k_t.size(0) != n[0] || k_t.size(1) != n[1] || k_t.size(3) != n[3] || n[2] % k_t.size(2) != 0)
+            raise(PyExc_ValueError, "k: shape " + text(k_t.sizes()) + " does not go with q of " + text(n));
+        if (v_t.size(0) != n[0] || v_t.size(1) != n[1] || v_t.size(2) != k_t.size(2))
+            raise(PyExc_ValueError, "v: shape " + text(v_t.sizes()) + " does not go with k of " + text(k_t.sizes()));
+        gh = integer(gh_); gw = integer(gw_);
+        if (n[1] != (int64_t)gh * gw) raise(PyExc_ValueError, "q: L != grid_h*grid_w");
+        B = (int)n[0]; L = (int)n[1]; H = (int)n[2]; Hk = (int)k_t.size(2); dk = (int)n[3]; dv = (int)v_t.size(3);
+        decay = numbers(a[3], H, "log_decay");
+    }
+    std::vector<int64_t> state() const { return {B, H, dk, dv}; }
+    const int *lengths(PyObject *o) const { return (const int *)dev_opt(o, ScalarType::Int, {B}, "lengths", q_t); }
+    Ws space(PyObject *o, int backward) const
+    {
+        return workspace(o, none(o) ? dig_decay_workspace_bytes(B, H, Hk, gh, gw, dk, dv, dtype, backward) : 0, q_t);
+    }
+};
+
+// q k v log_decay grid_h grid_w direction s_in lengths want_s_out out workspace
+PyObject *decay_fwd(PyObject *const *a)
+{
+    const Decay g(a, a[4], a[5]);
+    const On on(g.q_t);
+    const int dir = integer(a[6]);
+    const float *si = (const float *)dev_opt(a[7], kF32, g.state(), "s_in", g.q_t);
+    const int *len = g.lengths(a[8]);
+    const std::vector<int64_t> shape = {g.B, g.L, g.H, g.dv};
+    Tensor out = given(a[10], shape, g.st, g.q_t, "out"), so;
+    void *op = dev(out, g.st, shape, "out", g.q_t);
+    if (truth(a[9])) so = empty(g.state(), kF32, g.q_t);
+    const Ws w = g.space(a[11], 0);
+    float *sop = so.defined() ? (float *)so.data_ptr() : nullptr;
+    void *s = on.stream();
+    CALL(dig_decay_fwd(g.q, g.k, g.v, g.strides, g.decay.data(), len, si, op, sop, g.B, g.H, g.Hk, g.gh, g.gw, g.dk, g.dv, dir, g.dtype, w.p, w.n, s), "dig_decay_fwd");
+    return pack({out, so});
+}
+
+// q k v log_decay d_out grid_h grid_w direction s_in ds_out lengths want_ds_in grads workspace
+PyObject *decay_bwd(PyObject *const *a)
+{
+    const Decay g(a, a[5], a[6]);
+    const On on(g.q_t);
+    const int dir = integer(a[7]);
+    const std::vector<int64_t> ks = {g.B, g.L, g.Hk, g.dk}, vs = {g.B, g.L, g.Hk, g.dv};
+    const void *gp = dev(a[4], g.st, {g.B, g.L, g.H, g.dv}, "d_out", g.q_t);
+    const float *si = (const float *)dev_opt(a[8], kF32, g.state(), "s_in", g.q_t), *dso = (const float *)dev_opt(a[9], kF32, g.state(), "ds_out", g.q_t);
+    const int *len = g.lengths(a[10]);
+    Tensor dq, dk, dv, dsi;
+    if (none(a[12])) {
+        dq = empty(g.q_t.sizes(), g.st, g.q_t);
+        dk = empty(ks, g.st, g.q_t);
+        dv = empty(vs, g.st, g.q_t);
+    } else {
+        PyObject *seq = PySequence_Fast(a[12], "grads: need (dq, dk, dv)");
+        if (!seq) throw Raised{};
+        PyObject **it = PySequence_Fast_ITEMS(seq);
+        const bool three = PySequence_Fast_GET_SIZE(seq) == 3 && THPVariable_Check(it[0]) && THPVariable_Check(it[1]) && THPVariable_Check(it[2]);
+        if (three) {
+            dq = THPVariable_Unpack(it[0]);
+            dk = THPVariable_Unpack(it[1]);
+            dv = THPVariable_Unpack(it[2]);
+        }
+        Py_DECREF(seq);
+        if (!three) raise(PyExc_ValueError, "grads: need three tensors (dq, dk, dv)");
+    }
+    void *qp = dev(dq, g.st, g.q_t.sizes(), "dq", g.q_t), *kp = dev(dk, g.st, ks, "dk", g.q_t), *vp = dev(dv, g.st, vs, "dv", g.q_t);
+    if (truth(a[11])) dsi = empty(g.state(), kF32, g.q_t);
+    const Ws w = g.space(a[13], 1);
+    float *dsip = dsi.defined() ? (float *)dsi.data_ptr() : nullptr;
+    void *s = on.stream();
+    CALL(dig_decay_bwd(g.q, g.k, g.v, g.strides, g.decay.data(), len, gp, si, dso, qp, kp, vp, dsip, g.B, g.H, g.Hk, g.gh, g.gw, g.dk, g.dv, dir, g.dtype, w.p, w.n, s),
+         "dig_decay_bwd");
+    return pack({dq, dk, dv, dsi});
+}
+
+// q k v log_decay state out
+PyObject *decay_step(PyObject *const *a)
+{
+    const Tensor &q = tensor(a[0], "q"), &k = tensor(a[1], "k"), &v = tensor(a[2], "v");
+    if (q.dim() != 3) raise(PyExc_ValueError, "q: need 3 dimensions [B, H, d_k], got shape " + text(q.sizes()));
+    if (k.dim() != 3 || k.size(1) < 1 || q.size(1) % k.size(1) != 0) raise(PyExc_ValueError, "k: shape " + text(k.sizes()) + " does not go with q of " + text(q.sizes()));
+    if (v.dim() != 3) raise(PyExc_ValueError, "v: need 3 dimensions [B, H_kv, d_v], got shape " + text(v.sizes()));
+    const int64_t B = q.size(0), H = q.size(1), Hk = k.size(1), dk = q.size(2), dv = v.size(2);
+    const int dtype = dtype_of(q, false);
+    const ScalarType st = storage(dtype);
+    const void *qp = dev(q, st, "q"), *kp = dev(k, st, {B, Hk, dk}, "k", q), *vp = dev(v, st, {B, Hk, dv}, "v", q);
+    const On on(q);
+    const std::vector<float> decay = numbers(a[3], H, "log_decay");
+    float *sp = (float *)dev(a[4], kF32, {B, H, dk, dv}, "state", q);
+    const std::vector<int64_t> shape = {B, H, dv};
+    Tensor out = given(a[5], shape, st, q, "out");
+    void *op = dev(out, st, shape, "out", q), *s = on.stream();
+    CALL(dig_decay_step(qp, kp, vp, decay.data(), sp, op, sp, (int)B, (int)H, (int)Hk, (int)dk, (int)dv, dtype, s), "dig_decay_step");
+    return wrap(out);
+}
+
+// q k positions freqs axes interleaved inverse inplace
+PyObject *rope(PyObject *const *a)
+{
+    const Tensor &q = tensor(a[0], "q"), &pos = tensor(a[2], "positions");
+    const int dtype = dtype_of(q, false);
+    const ScalarType st = storage(dtype);
+    long long strides[4] = {0, 0, 0, 0};
+    const void *qp = rows(q, st, "q", q, strides), *kp = nullptr;
+    const int64_t B = q.size(0), L = q.size(1), d = q.size(3);
+    const On on(q);
+    int Hk = 0;
+    if (!none(a[1])) {
+        const Tensor &k = tensor(a[1], "k");
+        kp = rows(k, st, "k", q, strides + 2);
+        if (k.size(0) != B || k.size(1) != L || k.size(3) != d) raise(PyExc_ValueError, "k: shape " + text(k.sizes()) + " does not go with q of " + text(q.sizes()));
+        Hk = (int)k.size(2);
+    }
+    const bool batched = pos.dim() == 3;
+    if (!(pos.dim() == 2 || (batched && pos.size(0) == B)) || pos.size(-2) != L) raise(PyExc_ValueError, "positions: need [L, axes] or [B, L, axes], got shape " + text(pos.sizes()));
+    const int *pp = (const int *)dev(pos, ScalarType::Int, pos.sizes(), "positions", q);
+    std::vector<double> freqs;
+    std::vector<int> axes;
+    for (int which = 0; which < 2; ++which) {
+        PyObject *seq = PySequence_Fast(a[3 + which], which ? "axes: need a sequence of integers" : "freqs: need a sequence of numbers");
+        if (!seq) throw Raised{};
+        const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq);
+        bool bad = false;
+        for (Py_ssize_t i = 0; i < n && !bad; ++i) {
+            PyObject *o = PySequence_Fast_GET_ITEM(seq, i);
+            if (which) {
+                const long v = PyLong_AsLong(o);
+                bad = v == -1 && PyErr_Occurred();
+                axes.push_back(v < 0 || v > 255 ? -1 : (int)v);
+            } else {
+                freqs.push_back(PyFloat_AsDouble(o));
+                bad = freqs.back() == -1.0 && PyErr_Occurred();
+            }
+        }
+        Py_DECREF(seq);
+        if (bad) throw Raised{};
+    }
+    if (freqs.size() != axes.size()) raise(PyExc_ValueError, "freqs and axes: " + std::to_string(freqs.size()) + " and " + std::to_string(axes.size()) + " values");
+    const bool in_place = truth(a[7]);
+    Tensor qo = in_place ? q : empty(q.sizes(), st, q), ko;
+    if (kp) ko = in_place ? tensor(a[1], "k") : empty(tensor(a[1], "k").sizes(), st, q);
+    const int inter = truth(a[5]), inv = truth(a[6]);
+    void *qop = qo.data_ptr(), *kop = kp ? ko.data_ptr() : nullptr, *s = on.stream();
+    if (in_place)           // rows that coincide cannot all be written
+        for (int i = 0; i < (kp ? 2 : 1); ++i) {
+            const Tensor &t = i ? ko : qo;
+            if (!t.is_non_overlapping_and_dense() && ((B > 1 && t.stride(0) < (L - 1) * strides[2 * i + 1] + t.size(2) * d && t.stride(1) < (B - 1) * strides[2 * i] + t.size(2) * d) || (L > 1 && t.stride(1) < t.size(2) * d)))
+                raise(PyExc_ValueError, std::string(i ? "k" : "q") + ": rows overlap, they cannot be turned in place");
+        }
+    CALL(dig_rope(qp, kp, strides, pp, batched ? (int)B : 1, (int)pos.size(-1), freqs.data(), axes.data(), (int)freqs.size(), qop, kop, (int)B, (int)L, (int)q.size(2), Hk,
+                  (int)d, inter, inv, dtype, s), "dig_rope");
+    return pack({qo, ko});
+}
+
+// Groups of an affine parameter [D] or [groups, D].
+int groups_of(const Tensor &t, int D, const char *name)
+{
+    if ((t.dim() != 1 && t.dim() != 2) || t.size(-1) != D || t.numel() == 0)
+        raise(PyExc_ValueError, std::string(name) + ": need [" + std::to_string(D) + "] or [groups, " + std::to_string(D) + "], got shape " + text(t.sizes()));
+    return t.dim() == 1 ? 1 : (int)t.size(0);
+}
+// x w b eps
+PyObject *layernorm_fwd(PyObject *const *a)
+{
+    const Tensor &x = tensor(a[0], "x");
+    int D, groups = 1;
+    long long rows;
+    if (x.dim() < 1 || x.numel() == 0) raise(PyExc_ValueError, "x: need rows of at least one value, got shape " + text(x.sizes()));
+    rows_of(x, D, rows);
+    const int dtype = dtype_of(x, false);
+    const ScalarType st = storage(dtype);
+    const void *xp = dev(x, st, "x");
+    const On on(x);
+    const float *wp = nullptr, *bp = nullptr;
+    if (!none(a[1])) {
+        const Tensor &w = tensor(a[1], "w");
+        groups = groups_of(w, D, "w");
+        wp = (const float *)dev(w, kF32, w.sizes(), "w", x);
+    }
+    if (!none(a[2])) {
+        const Tensor &b = tensor(a[2], "b");
+        const int g = groups_of(b, D, "b");
+        if (wp && g != groups) raise(PyExc_ValueError, "b: shape " + text(b.sizes()) + " does not go with w of " + text(tensor(a[1], "w").sizes()));
+        groups = g;
+        bp = (const float *)dev(b, kF32, b.sizes(), "b", x);
+    }
+    if (rows % groups) raise(PyExc_ValueError, "x: " + std::to_string(rows) + " rows in " + std::to_string(groups) + " groups");
+    const float eps = real(a[3]);
+    Tensor y = empty(x.sizes(), st, x);
+    void *yp = y.data_ptr(), *s = on.stream();
+    CALL(dig_layernorm_fwd(xp, wp, bp, yp, rows, groups, D, eps, dtype, s), "dig_layernorm_fwd");
+    return wrap(y);
+}
+// x dy w eps affine_grads workspace
+PyObject *layernorm_bwd(PyObject *const *a)
+{
+    const Tensor &x = tensor(a[0], "x");
+    int D, groups = 1;
+    long long rows;
+    if (x.dim() < 1 || x.numel() == 0) raise(PyExc_ValueError, "x: need rows of at least one value, got shape " + text(x.sizes()));
+    rows_of(x, D, rows);
+    const int dtype = dtype_of(x, false);
+    const ScalarType st = storage(dtype);
+    const void *xp = dev(x, st, "x"), *gp = dev(a[1], st, x.sizes(), "dy", x);
+    const On on(x);
+    const float *wp = nullptr;
+    std::vector<int64_t> shape = {D};
+    if (!none(a[2])) {
+        const Tensor &w = tensor(a[2], "w");
+        groups = groups_of(w, D, "w");
+        shape = w.sizes().vec();
+        wp = (const float *)dev(w, kF32, shape, "w", x);
+    }
+    if (rows % groups) raise(PyExc_ValueError, "x: " + std::to_string(rows) + " rows in " + std::to_string(groups) + " groups");
+    const float eps = real(a[3]);
+    Tensor dx = empty(x.sizes(), st, x), dw, db;
+    Ws w;
+    if (truth(a[4])) {
+        dw = empty(shape, kF32, x);
+        db = empty(shape, kF32, x);
+        w = workspace(a[5], none(a[5]) ? dig_layernorm_bwd_workspace_bytes(rows, groups, D) : 0, x);
+    }
+    void *dxp = dx.data_ptr(), *s = on.stream();
+    float *dwp = dw.defined() ? (float *)dw.data_ptr() : nullptr, *dbp = db.defined() ? (float *)db.data_ptr() : nullptr;
+    CALL(dig_layernorm_bwd(xp, gp, wp, dxp, dwp, dbp, rows, groups, D, eps, dtype, w.p, w.n, s), "dig_layernorm_bwd");
+    return pack({dx, dw, db});
+}
+
 template <PyObject *(*F)(PyObject *const *), int N>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -516,6 +809,7 @@ PyMethodDef kMethods[] = {
     FAST(gate_logsigmoid, 3), FAST(gla_fwd, 11), FAST(gla_bwd, 12), FAST(gla_fwd_state, 12), FAST(gla_bwd_state, 13),
     FAST(gla_fwd_multi, 11), FAST(gla_bwd_multi, 12), FAST(gla_fwd_beta, 11), FAST(gla_bwd_beta, 12), FAST(gla_fwd_outgate, 15),
     FAST(outgate_fwd, 6), FAST(outgate_bwd, 9), FAST(dwconv, 8), FAST(dwconv_bwd, 9),
+    FAST(decay_fwd, 12), FAST(decay_bwd, 14), FAST(decay_step, 6), FAST(rope, 8), FAST(layernorm_fwd, 4), FAST(layernorm_bwd, 6),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 

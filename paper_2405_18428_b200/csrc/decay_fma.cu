@@ -1,0 +1,168 @@
+// Linear attention with a decay for each head in fp32 arithmetic (equations in decay.cuh): one CTA per segment of a sequence walks
+// over tiles of 64 positions with the state in shared memory.  Serves fp32 storage, whose products have to be fp32-accurate.
+#include "decay.cuh"
+
+namespace dig {
+namespace decay {
+namespace {
+
+constexpr int T = kTileFma, NT = 256, LDP = T + 4;
+
+// Rows of a tile as fp32 in shared memory, stride d + 4 floats (a step of one row is a step of 4 banks); rows behind the end zero.
+template <typename S>
+__device__ __forceinline__ void load_rows(float *dst, const Args &a, const Rows &r, int d, int dir, int b, int h, int p0, int n)
+{
+    const S *base = (const S *)r.p + (size_t)b * r.batch + (size_t)(h / r.share) * d;
+    for (int i = threadIdx.x; i < T * (d / 4); i += NT) {
+        const int row = i / (d / 4), c = (i - row * (d / 4)) * 4, p = p0 + row;
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (p < n) x = load4(base + (size_t)token_at(a, dir, p, n) * r.token + c);
+        *reinterpret_cast<float4 *>(dst + row * (d + 4) + c) = x;
+    }
+}
+
+__device__ __forceinline__ float dot4(float4 x, float4 y, float s) { return fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s)))); }
+__device__ __forceinline__ void axpy4(float4 &s, float w, float4 x)
+{
+    s.x = fmaf(w, x.x, s.x); s.y = fmaf(w, x.y, s.y); s.z = fmaf(w, x.z, s.z); s.w = fmaf(w, x.w, s.w);
+}
+__device__ __forceinline__ float4 scaled(float4 x, float w) { return make_float4(x.x * w, x.y * w, x.z * w, x.w * w); }
+
+template <typename S, bool LOCAL>
+__global__ void __launch_bounds__(NT) decay_fma(const __grid_constant__ Args a)
+{
+    extern __shared__ float4 smem4[];
+    float *sm = reinterpret_cast<float *>(smem4);
+    const Pass &ps = a.pass[blockIdx.z];
+    const int seg = blockIdx.x, bh = blockIdx.y, b = bh / a.H, h = bh - b * a.H, dk = ps.dk, dv = ps.dv, ldk = dk + 4, ldv = dv + 4;
+    float *X = sm, *K = X + dk * ldv, *V = K + T * ldk, *pw = V + T * ldv, *Q = pw + T + 4, *P = Q + T * ldk;
+    const float lam = a.lam.v[h];
+    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+    if (tid <= T) pw[tid] = exp2_of(lam * tid);
+    pdl_wait();
+    const int n = length_of(a.lengths, a.L, b);
+    const size_t dd = (size_t)dk * dv;
+    float *local = ps.local + ((size_t)bh * a.nseg + seg) * dd;
+    const float *x0 = LOCAL ? nullptr : seg > 0 ? local : ps.x0 ? ps.x0 + (size_t)bh * dd : nullptr;
+    const bool turned = seg > 0 ? ps.local_transposed : ps.x_transposed;
+    for (int i = tid; i < dk * dv; i += NT) {
+        const int r = i / dv, c = i - r * dv;
+        X[r * ldv + c] = x0 ? x0[turned ? c * dk + r : i] : 0.f;
+    }
+    const int tiles = (a.L + T - 1) / T, t1 = min((seg + 1) * a.G, tiles);
+    for (int t = seg * a.G; t < t1; ++t) {
+        const int p0 = t * T, rows = min(T, n - p0), lead = p0 == 0 ? ps.first : 1;
+        __syncthreads();
+        if (rows > 0) {
+            load_rows<S>(K, a, ps.k, dk, ps.dir, b, h, p0, n);
+            load_rows<S>(V, a, ps.v, dv, ps.dir, b, h, p0, n);
+            if (!LOCAL) load_rows<S>(Q, a, ps.q, dk, ps.dir, b, h, p0, n);
+        }
+        __syncthreads();
+        if (!LOCAL) {
+            if (rows > 0) {
+                float s[4][4] = {};
+                for (int c = 0; c < dk; c += 4) {
+                    float4 qv[4], kv[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        qv[i] = *reinterpret_cast<const float4 *>(Q + (ty + 16 * i) * ldk + c);
+                        kv[i] = *reinterpret_cast<const float4 *>(K + (tx + 16 * i) * ldk + c);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) s[i][j] = dot4(qv[i], kv[j], s[i][j]);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int r = ty + 16 * i, c = tx + 16 * j;
+                        P[r * LDP + c] = r >= c ? s[i][j] * pw[r - c] : 0.f;
+                    }
+            }
+            __syncthreads();
+            const size_t tok = (size_t)a.H * dv;
+            for (int c = tx * 4; c < dv; c += 64) {
+                float4 o[4] = {}, e[4] = {};
+                if (rows > 0) {
+                    // rows of one thread are 16 apart: nothing above the last of them counts
+                    for (int j = 0; j < T; ++j) {
+                        const float4 x = *reinterpret_cast<const float4 *>(V + j * ldv + c);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) if (j <= ty + 16 * i) axpy4(o[i], P[(ty + 16 * i) * LDP + j], x);
+                    }
+                    for (int j = 0; j < dk; ++j) {
+                        const float4 x = *reinterpret_cast<const float4 *>(X + j * ldv + c);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) axpy4(e[i], Q[(ty + 16 * i) * ldk + j], x);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = ty + 16 * i, p = p0 + r;
+                    if (p >= a.L) continue;
+                    if (p < n) axpy4(o[i], pw[r] * (lead ? pw[1] : 1.f), e[i]);
+                    const size_t at = ((size_t)b * a.L + token_at(a, ps.dir, p, n)) * tok + (size_t)h * dv + c;
+                    const float4 y = p < n ? o[i] : make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (ps.out_f32) store4((float *)ps.out + at, y);
+                    else store4((S *)ps.out + at, y);
+                }
+            }
+            __syncthreads();
+        }
+        if (rows <= 0) continue;
+        const float whole = pw[rows - 1] * (lead ? pw[1] : 1.f);
+        for (int r0 = ty * 4; r0 < dk; r0 += 64)
+            for (int c = tx * 4; c < dv; c += 64) {
+                float4 x[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = scaled(*reinterpret_cast<const float4 *>(X + (r0 + i) * ldv + c), whole);
+                for (int j = 0; j < rows; ++j) {
+                    const float4 kv = scaled(*reinterpret_cast<const float4 *>(K + j * ldk + r0), pw[rows - 1 - j]);
+                    const float4 vv = *reinterpret_cast<const float4 *>(V + j * ldv + c);
+                    axpy4(x[0], kv.x, vv); axpy4(x[1], kv.y, vv); axpy4(x[2], kv.z, vv); axpy4(x[3], kv.w, vv);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) *reinterpret_cast<float4 *>(X + (r0 + i) * ldv + c) = x[i];
+            }
+    }
+    __syncthreads();
+    if (LOCAL) {
+        for (int i = tid; i < dk * dv; i += NT) local[i] = X[i / dv * ldv + i % dv];
+    } else if (ps.x_end && a.nseg == 1) {
+        const float f = n > 0 && ps.last ? pw[1] : 1.f;          // no token: the start state
+        for (int i = tid; i < dk * dv; i += NT) ps.x_end[(size_t)bh * dd + i] = X[i / dv * ldv + i % dv] * f;
+    }
+    pdl_launch_dependents();
+}
+
+size_t smem_bytes(int dk, int dv, bool local)
+{
+    const size_t f = (size_t)dk * (dv + 4) + (size_t)T * (dk + 4 + dv + 4) + T + 4 + (local ? 0 : (size_t)T * (dk + 4) + T * LDP);
+    return f * 4;
+}
+
+template <typename S, bool LOCAL>
+dig_status launch(const Args &a, cudaStream_t stream)
+{
+    int segs = a.nseg;
+    size_t smem = 0;
+    for (int i = 0; i < a.passes; ++i) smem = smem > smem_bytes(a.pass[i].dk, a.pass[i].dv, LOCAL) ? smem : smem_bytes(a.pass[i].dk, a.pass[i].dv, LOCAL);
+    dig_status st = ensure_dynamic_smem((const void *)decay_fma<S, LOCAL>, smem);
+    if (st != DIG_OK) return st;
+    KernelTimer t(LOCAL ? KID_DECAY_LOCAL : KID_DECAY, stream);
+    return cuda_ok(launch_pdl(decay_fma<S, LOCAL>, dim3(segs, a.B * a.H, a.passes), dim3(NT), smem, stream, a));
+}
+
+}  // namespace
+
+dig_status fma_pass(const Args &a, bool local, int dtype, cudaStream_t stream)
+{
+    if (dtype == DIG_F32) return local ? launch<float, true>(a, stream) : launch<float, false>(a, stream);
+    return local ? launch<__nv_bfloat16, true>(a, stream) : launch<__nv_bfloat16, false>(a, stream);
+}
+
+}  // namespace decay
+}  // namespace dig

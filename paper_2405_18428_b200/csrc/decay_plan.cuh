@@ -1,0 +1,88 @@
+// Host side of linear attention with a decay for each head: how sequences are cut, and the workspace that takes.  Plain arithmetic
+// without CUDA calls.
+#pragma once
+
+#include <cmath>
+
+#include "decay.cuh"
+
+namespace dig {
+
+// Arguments of a whole-sequence call, checked by the entry point.
+struct DecayCall {
+    const void *q, *k, *v;
+    const long long *strides;            // batch and token strides of q, k, v, or null: dense
+    const float *log_decay;
+    const int *lengths;
+    const float *s_in, *ds_out;
+    const void *d_out;
+    void *out, *dq, *dk_out, *dv_out;
+    float *s_out, *ds_in;
+    int B, H, H_kv, L, gh, gw, dk, dv, dir, dtype;
+    void *ws;
+    cudaStream_t stream;
+};
+
+namespace decay {
+
+struct Plan {
+    int tile, nseg, G;
+};
+// One CTA per sequence and pass where that fills the machine; else as many segments as give every SM its CTAs.
+inline Plan make_plan(int B, int H, int L, int passes, int dtype)
+{
+    Plan p;
+    p.tile = kTileFma;
+    const long long tiles = (L + p.tile - 1) / p.tile, seqs = (long long)B * H * passes, room = 2ll * kSms;
+    long long nseg = seqs * 2 > room ? 1 : room / seqs;
+    if (nseg > tiles) nseg = tiles;
+    p.G = (int)((tiles + nseg - 1) / nseg);
+    p.nseg = (int)((tiles + p.G - 1) / p.G);
+    (void)dtype;
+    return p;
+}
+
+// Workspace, every block 256-byte aligned: states of the segments, [B*H][nseg][dk][dv] fp32 (backward: twice), and where heads share
+// keys and values the gradients of each head before they are summed, fp32 [B][L][H][d].
+struct Carved {
+    Plan plan;
+    float *local[2], *part_k, *part_v;
+    size_t bytes;
+};
+inline Carved carve(char *base, int B, int H, int H_kv, int L, int dk, int dv, int dtype, bool backward)
+{
+    Carved w{};
+    w.plan = make_plan(B, H, L, backward ? 3 : 1, dtype);
+    size_t o = 0;
+    auto take = [&](size_t bytes) { char *p = base + o; o += align256(bytes); return reinterpret_cast<float *>(p); };
+    const size_t state = w.plan.nseg > 1 ? (size_t)B * H * w.plan.nseg * dk * dv * 4 : 16;
+    w.local[0] = take(state);
+    if (backward) {
+        w.local[1] = take(state);
+        if (H != H_kv) {
+            w.part_k = take((size_t)B * L * H * dk * 4);
+            w.part_v = take((size_t)B * L * H * dv * 4);
+        }
+    }
+    w.bytes = o;
+    return w;
+}
+
+// log2 of the decays; false where one is no decay: above 0 or no finite number.
+inline bool set_decay(Log2Decay &l, const float *log_decay, int H)
+{
+    for (int h = 0; h < H; ++h) {
+        const float x = log_decay[h];
+        if (!(x <= 0.f) || std::isinf(x)) return false;
+        l.v[h] = (float)std::fmax(x * 1.4426950408889634, -1e6);          // 2^-1e6 is 0 as well, and its multiples are finite
+    }
+    return true;
+}
+
+inline dig_status pass_kernel(const Args &a, bool local, int dtype, cudaStream_t stream)
+{
+    return fma_pass(a, local, dtype, stream);
+}
+
+}  // namespace decay
+}  // namespace dig

@@ -6,6 +6,7 @@
 #include <utility>
 #include <vector>
 
+#include "decay_plan.cuh"
 #include "dig_common.cuh"
 #include "sweep.cuh"
 #include "umma.cuh"
@@ -27,6 +28,20 @@ dig_status launch_outgate_bwd(const void *o, const void *r, const void *dz, cons
 size_t dwconv_bwd_workspace_bytes(int B, int gh, int gw, int D);
 dig_status launch_dwconv_bwd(const void *x, const void *w, const void *dy, void *dx, float *dw, float *dbias,
                              int B, int gh, int gw, int D, int dir, int dtype, float *partial, cudaStream_t stream);
+
+size_t decay_workspace_bytes(int B, int H, int H_kv, int L, int dk, int dv, int dtype, bool backward);
+dig_status decay_fwd_launch(const DecayCall &c);
+dig_status decay_bwd_launch(const DecayCall &c);
+dig_status decay_step_launch(const void *q, const void *k, const void *v, const float *log_decay, const float *s_in, void *out, float *s_out,
+                             int B, int H, int H_kv, int dk, int dv, int dtype, cudaStream_t stream);
+dig_status launch_rope(const void *q, const void *k, const long long *strides, const int *positions, int pos_batches, int n_axes,
+                       const double *freqs, const int *axes, int n_pairs, void *q_out, void *k_out, int B, int L, int H, int H_k, int d,
+                       bool interleaved, bool inverse, int dtype, cudaStream_t stream);
+dig_status launch_layernorm_fwd(const void *x, const float *w, const float *b, void *y, long long rows, int groups, int D, float eps, int dtype,
+                                cudaStream_t stream);
+size_t layernorm_bwd_workspace_bytes(long long rows, int groups, int D);
+dig_status launch_layernorm_bwd(const void *x, const void *dy, const float *w, void *dx, float *dw, float *db, long long rows, int groups, int D,
+                                float eps, int dtype, float *partial, cudaStream_t stream);
 
 namespace {
 
@@ -86,7 +101,8 @@ const char *const kKernelNames[KID_COUNT] = {
     "gate_logsigmoid", "srem_dwconv3x3", "srem_dwconv_wgrad", "gla_outgate", "state_scan_fwd", "state_scan_bwd",
     "fma_chunk_state", "fma_chunk_out", "fma_chunk_bwd",
     "mma_chunk_state", "mma_chunk_out", "mma_chunk_bwd",
-    "sweep_local", "seg_scan", "sweep_fwd", "sweep_bwd"};
+    "sweep_local", "seg_scan", "sweep_fwd", "sweep_bwd",
+    "decay_local", "decay_scan", "decay_pass", "decay_share_sum", "decay_step", "rope", "layernorm_fwd", "layernorm_bwd", "layernorm_sum"};
 struct Profile {
     bool on = false;
     std::vector<cudaEvent_t> ev;      // 2 per timed launch, created lazily and reused
@@ -483,6 +499,121 @@ dig_status dig_gla_bwd_multi(const void *q, const void *k, const void *v, const 
     a.dtype = dtype;
     a.stream = (cudaStream_t)cuda_stream;
     return sweep_gla_bwd_multi(a, direction_mask);
+}
+
+// ---- linear attention with a decay for each head ------------------------------------------------------------------
+static bool decay_sizes_ok(int B, int H, int H_kv, int d_k, int d_v, int dtype)
+{
+    return B > 0 && H > 0 && H <= decay::kMaxHeads && H_kv > 0 && H % H_kv == 0 && (long long)B * H <= 65535 && valid_dim(d_k) && valid_dim(d_v) &&
+           (dtype == DIG_F32 || dtype == DIG_BF16);
+}
+static bool decay_geometry_ok(int B, int H, int H_kv, int grid_h, int grid_w, int d_k, int d_v, int dtype)
+{
+    return grid_h > 0 && grid_w > 0 && (long long)grid_h * grid_w <= (1ll << 24) && decay_sizes_ok(B, H, H_kv, d_k, d_v, dtype);
+}
+// Strides keep every row on a 16-byte boundary; inputs only, so rows may coincide.
+static bool strides_ok(const long long *s, int n, int dtype)
+{
+    const int unit = dtype == DIG_F32 ? 4 : 8;
+    for (int i = 0; s && i < n; ++i)
+        if (s[i] < 0 || s[i] % unit != 0) return false;
+    return true;
+}
+
+size_t dig_decay_workspace_bytes(int B, int H, int H_kv, int grid_h, int grid_w, int d_k, int d_v, int dtype, int backward)
+{
+    if (!decay_geometry_ok(B, H, H_kv, grid_h, grid_w, d_k, d_v, dtype)) return 0;
+    return decay_workspace_bytes(B, H, H_kv, grid_h * grid_w, d_k, d_v, dtype, backward != 0);
+}
+
+dig_status dig_decay_fwd(const void *q, const void *k, const void *v, const long long *strides, const float *log_decay_per_head,
+                         const int *lengths, const float *s_in, void *out, float *s_out, int B, int H, int H_kv, int grid_h, int grid_w,
+                         int d_k, int d_v, int direction, int dtype, void *workspace, size_t workspace_bytes, void *cuda_stream)
+{
+    if (!q || !k || !v || !log_decay_per_head || !out) return DIG_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(s_in) || !aligned16(s_out)) return DIG_ERR_INVALID_ARG;
+    if (!decay_geometry_ok(B, H, H_kv, grid_h, grid_w, d_k, d_v, dtype) || direction < 0 || direction > 3) return DIG_ERR_INVALID_ARG;
+    if (!strides_ok(strides, 6, dtype) || (reinterpret_cast<uintptr_t>(lengths) & 3u) != 0) return DIG_ERR_INVALID_ARG;
+    if (lengths && (direction & 2)) return DIG_ERR_UNSUPPORTED;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < decay_workspace_bytes(B, H, H_kv, grid_h * grid_w, d_k, d_v, dtype, false)) return DIG_ERR_WORKSPACE;
+    DecayCall c{};
+    c.q = q; c.k = k; c.v = v; c.strides = strides; c.log_decay = log_decay_per_head; c.lengths = lengths; c.s_in = s_in; c.out = out; c.s_out = s_out;
+    c.B = B; c.H = H; c.H_kv = H_kv; c.L = grid_h * grid_w; c.gh = grid_h; c.gw = grid_w; c.dk = d_k; c.dv = d_v; c.dir = direction; c.dtype = dtype;
+    c.ws = workspace; c.stream = (cudaStream_t)cuda_stream;
+    return decay_fwd_launch(c);
+}
+
+dig_status dig_decay_bwd(const void *q, const void *k, const void *v, const long long *strides, const float *log_decay_per_head,
+                         const int *lengths, const void *d_out, const float *s_in, const float *ds_out, void *dq, void *dk, void *dv,
+                         float *ds_in, int B, int H, int H_kv, int grid_h, int grid_w, int d_k, int d_v, int direction, int dtype,
+                         void *workspace, size_t workspace_bytes, void *cuda_stream)
+{
+    if (!q || !k || !v || !log_decay_per_head || !d_out || !dq || !dk || !dv) return DIG_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(d_out) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv) || !aligned16(s_in) ||
+        !aligned16(ds_out) || !aligned16(ds_in))
+        return DIG_ERR_INVALID_ARG;
+    if (!decay_geometry_ok(B, H, H_kv, grid_h, grid_w, d_k, d_v, dtype) || direction < 0 || direction > 3) return DIG_ERR_INVALID_ARG;
+    if (!strides_ok(strides, 6, dtype) || (reinterpret_cast<uintptr_t>(lengths) & 3u) != 0) return DIG_ERR_INVALID_ARG;
+    if (lengths && (direction & 2)) return DIG_ERR_UNSUPPORTED;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < decay_workspace_bytes(B, H, H_kv, grid_h * grid_w, d_k, d_v, dtype, true)) return DIG_ERR_WORKSPACE;
+    DecayCall c{};
+    c.q = q; c.k = k; c.v = v; c.strides = strides; c.log_decay = log_decay_per_head; c.lengths = lengths; c.d_out = d_out; c.s_in = s_in; c.ds_out = ds_out;
+    c.dq = dq; c.dk_out = dk; c.dv_out = dv; c.ds_in = ds_in;
+    c.B = B; c.H = H; c.H_kv = H_kv; c.L = grid_h * grid_w; c.gh = grid_h; c.gw = grid_w; c.dk = d_k; c.dv = d_v; c.dir = direction; c.dtype = dtype;
+    c.ws = workspace; c.stream = (cudaStream_t)cuda_stream;
+    return decay_bwd_launch(c);
+}
+
+dig_status dig_decay_step(const void *q, const void *k, const void *v, const float *log_decay_per_head, const float *s_in, void *out, float *s_out,
+                          int B, int H, int H_kv, int d_k, int d_v, int dtype, void *cuda_stream)
+{
+    if (!q || !k || !v || !log_decay_per_head || !s_in || !out || !s_out) return DIG_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(s_in) || !aligned16(out) || !aligned16(s_out)) return DIG_ERR_INVALID_ARG;
+    if (!decay_sizes_ok(B, H, H_kv, d_k, d_v, dtype)) return DIG_ERR_INVALID_ARG;
+    return decay_step_launch(q, k, v, log_decay_per_head, s_in, out, s_out, B, H, H_kv, d_k, d_v, dtype, (cudaStream_t)cuda_stream);
+}
+
+// ---- rotary positions and layer norm -------------------------------------------------------------------------------
+dig_status dig_rope(const void *q, const void *k, const long long *strides, const int *positions, int pos_batches, int n_axes, const double *freqs,
+                    const int *axes, int n_pairs, void *q_out, void *k_out, int B, int L, int H, int H_k, int d, int interleaved, int inverse,
+                    int dtype, void *cuda_stream)
+{
+    if (!q || !positions || !freqs || !axes || !q_out || (k && !k_out) || (!k && k_out)) return DIG_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || (reinterpret_cast<uintptr_t>(positions) & 3u) != 0) return DIG_ERR_INVALID_ARG;
+    if (B <= 0 || L <= 0 || H <= 0 || (k && H_k <= 0) || !valid_dim(d) || (dtype != DIG_F32 && dtype != DIG_BF16)) return DIG_ERR_INVALID_ARG;
+    if (H > 65535 || H_k > 65535 || (long long)B * L > 0x7fffffffll) return DIG_ERR_UNSUPPORTED;
+    if ((pos_batches != 1 && pos_batches != B) || n_axes <= 0 || n_axes > 255 || n_pairs <= 0 || 2 * n_pairs > d || (d - 2 * n_pairs) % 4 != 0) return DIG_ERR_INVALID_ARG;
+    if (!strides_ok(strides, k ? 4 : 2, dtype)) return DIG_ERR_INVALID_ARG;
+    for (int i = 0; i < n_pairs; ++i)
+        if (axes[i] < 0 || axes[i] >= n_axes || !(freqs[i] >= -1e30 && freqs[i] <= 1e30)) return DIG_ERR_INVALID_ARG;
+    return launch_rope(q, k, strides, positions, pos_batches, n_axes, freqs, axes, n_pairs, q_out, k_out, B, L, H, H_k, d, interleaved != 0, inverse != 0, dtype,
+                       (cudaStream_t)cuda_stream);
+}
+
+static bool layernorm_sizes_ok(long long rows, int groups, int D, float eps)
+{
+    return rows > 0 && rows <= (1ll << 40) && groups > 0 && groups <= 65535 && rows % groups == 0 && D > 0 && D <= 8192 && eps >= 0.f;
+}
+
+dig_status dig_layernorm_fwd(const void *x, const float *w, const float *b, void *y, long long rows, int groups, int D, float eps, int dtype, void *cuda_stream)
+{
+    if (!x || !y || !aligned16(x) || !aligned16(y) || !aligned16(w) || !aligned16(b)) return DIG_ERR_INVALID_ARG;
+    if (!layernorm_sizes_ok(rows, groups, D, eps) || (dtype != DIG_F32 && dtype != DIG_BF16)) return DIG_ERR_INVALID_ARG;
+    return launch_layernorm_fwd(x, w, b, y, rows, groups, D, eps, dtype, (cudaStream_t)cuda_stream);
+}
+
+size_t dig_layernorm_bwd_workspace_bytes(long long rows, int groups, int D)
+{
+    return layernorm_sizes_ok(rows, groups, D, 0.f) ? layernorm_bwd_workspace_bytes(rows, groups, D) : 0;
+}
+
+dig_status dig_layernorm_bwd(const void *x, const void *dy, const float *w, void *dx, float *dw, float *db, long long rows, int groups, int D, float eps,
+                             int dtype, void *workspace, size_t workspace_bytes, void *cuda_stream)
+{
+    if (!x || !dy || !dx || !aligned16(x) || !aligned16(dy) || !aligned16(dx) || !aligned16(w) || !aligned16(dw) || !aligned16(db)) return DIG_ERR_INVALID_ARG;
+    if (!layernorm_sizes_ok(rows, groups, D, eps) || (dtype != DIG_F32 && dtype != DIG_BF16)) return DIG_ERR_INVALID_ARG;
+    if ((dw || db) && (!workspace || !aligned16(workspace) || workspace_bytes < layernorm_bwd_workspace_bytes(rows, groups, D))) return DIG_ERR_WORKSPACE;
+    return launch_layernorm_bwd(x, dy, w, dx, dw, db, rows, groups, D, eps, dtype, reinterpret_cast<float *>(workspace), (cudaStream_t)cuda_stream);
 }
 
 dig_status dig_last_device_status(void *cuda_stream)

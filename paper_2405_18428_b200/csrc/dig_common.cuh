@@ -182,6 +182,7 @@ enum KernelId {
     KID_FMA_STATE, KID_FMA_OUT, KID_FMA_BWD,
     KID_MMA_STATE, KID_MMA_OUT, KID_MMA_BWD,
     KID_SW_LOCAL, KID_SW_SCAN, KID_SW_FWD, KID_SW_BWD,
+    KID_DECAY_LOCAL, KID_DECAY_SCAN, KID_DECAY, KID_DECAY_SUM, KID_DECAY_STEP, KID_ROPE, KID_LN_FWD, KID_LN_BWD, KID_LN_SUM,
     KID_COUNT
 };
 struct KernelTimer {

@@ -29,7 +29,8 @@ EXPORTS = ("dig_set_impl", "dig_gla_query_impl", "dig_gla_workspace_bytes", "dig
            "dig_gla_fwd_multi", "dig_gla_bwd_multi", "dig_gla_multi_workspace_bytes",
            "dig_gla_fwd_beta", "dig_gla_bwd_beta", "dig_gla_beta_workspace_bytes", "dig_gla_fwd_outgate", "dig_srem_dwconv", "dig_srem_dwconv_bwd",
            "dig_srem_dwconv_bwd_workspace_bytes", "dig_gla_outgate_fwd", "dig_gla_outgate_bwd",
-           "dig_gla_outgate_bwd_workspace_bytes", "dig_last_device_status", "dig_selftest_wait_timeout",
+           "dig_gla_outgate_bwd_workspace_bytes", "dig_decay_workspace_bytes", "dig_decay_fwd", "dig_decay_bwd", "dig_decay_step",
+           "dig_rope", "dig_layernorm_fwd", "dig_layernorm_bwd", "dig_layernorm_bwd_workspace_bytes", "dig_last_device_status", "dig_selftest_wait_timeout",
            "dig_status_string", "dig_profile_enable", "dig_profile_kernels", "dig_profile_read")
 
 _lib = None
@@ -96,6 +97,22 @@ def lib() -> ctypes.CDLL:
         L.dig_gla_outgate_bwd_workspace_bytes.restype = ctypes.c_size_t
         L.dig_gla_outgate_bwd.argtypes = [vp] * 9 + [ll, i, fl, i, vp, ctypes.c_size_t, vp]
         L.dig_gla_outgate_bwd.restype = i
+        L.dig_decay_workspace_bytes.argtypes = [i] * 9
+        L.dig_decay_workspace_bytes.restype = sz
+        L.dig_decay_fwd.argtypes = [vp] * 9 + [i] * 9 + [vp, sz, vp]
+        L.dig_decay_fwd.restype = i
+        L.dig_decay_bwd.argtypes = [vp] * 13 + [i] * 9 + [vp, sz, vp]
+        L.dig_decay_bwd.restype = i
+        L.dig_decay_step.argtypes = [vp] * 7 + [i] * 6 + [vp]
+        L.dig_decay_step.restype = i
+        L.dig_rope.argtypes = [vp] * 4 + [i, i, vp, vp, i, vp, vp] + [i] * 8 + [vp]
+        L.dig_rope.restype = i
+        L.dig_layernorm_fwd.argtypes = [vp] * 4 + [ll, i, i, fl, i, vp]
+        L.dig_layernorm_fwd.restype = i
+        L.dig_layernorm_bwd_workspace_bytes.argtypes = [ll, i, i]
+        L.dig_layernorm_bwd_workspace_bytes.restype = sz
+        L.dig_layernorm_bwd.argtypes = [vp] * 6 + [ll, i, i, fl, i, vp, sz, vp]
+        L.dig_layernorm_bwd.restype = i
         L.dig_last_device_status.argtypes = [vp]
         L.dig_last_device_status.restype = i
         L.dig_selftest_wait_timeout.argtypes = [ctypes.c_uint, vp]
@@ -310,3 +327,57 @@ def dig_gla_fwd_outgate(q, k, v, gate, r, grid_h, grid_w, chunk=64, direction=DI
                         eps=1e-5, f32_out=False, want_out=True, workspace=None):
     """dig_gla_fwd and the output gate z = Swish(r) * LN(out) in one call; returns (out or None, z)."""
     return _binding().gla_fwd_outgate(q, k, v, gate, r, grid_h, grid_w, chunk, direction, ln_w, ln_b, eps, f32_out, want_out, workspace)
+
+
+def dig_decay_workspace_bytes(B, H, H_kv, grid_h, grid_w, d_k, d_v, dtype, backward) -> int:
+    return lib().dig_decay_workspace_bytes(B, H, H_kv, grid_h, grid_w, d_k, d_v, dtype, int(backward))
+
+
+def dig_decay_fwd(q, k, v, log_decay, grid_h, grid_w, direction=DIG_ROW_FWD, *, s_in=None, lengths=None, want_s_out=False, out=None,
+                  workspace=None):
+    """Linear attention with a decay for each head: S = exp(log_decay[h]) S + k^T v, out = q S; returns (out, s_out or None).
+
+    q: [B, L, H, d_k]; k: [B, L, H_kv, d_k]; v: [B, L, H_kv, d_v], H a multiple of H_kv; the last two dimensions dense, the others of any
+    stride (slices of a fused projection); log_decay: H numbers <= 0; s_in, s_out: fp32 [B, H, d_k, d_v]; lengths: int32 [B] tokens of
+    each sequence of a padded batch, whose rows of `out` behind the end are zeros (row orders only)."""
+    return _binding().decay_fwd(q, k, v, log_decay, grid_h, grid_w, direction, s_in, lengths, want_s_out, out, workspace)
+
+
+def dig_decay_bwd(q, k, v, log_decay, d_out, grid_h, grid_w, direction=DIG_ROW_FWD, *, s_in=None, ds_out=None, lengths=None,
+                  want_ds_in=False, grads=None, workspace=None):
+    """Returns (dq, dk, dv, ds_in or None) for the loss <d_out, out> + <ds_out, s_out>; `grads`: (dq, dk, dv) to write to."""
+    return _binding().decay_bwd(q, k, v, log_decay, d_out, grid_h, grid_w, direction, s_in, ds_out, lengths, want_ds_in, grads, workspace)
+
+
+def dig_decay_step(q, k, v, log_decay, state, *, out=None):
+    """One more token of every sequence: updates `state` (fp32 [B, H, d_k, d_v]) in place and returns out [B, H, d_v].
+
+    q: [B, H, d_k]; k: [B, H_kv, d_k]; v: [B, H_kv, d_v]; log_decay: H numbers <= 0."""
+    return _binding().decay_step(q, k, v, log_decay, state, out)
+
+
+def dig_rope_freqs(pairs_per_axis, theta=10000.0):
+    """Frequencies and axes for dig_rope: a ladder theta^(-i/n) of its own for each axis, n = pairs_per_axis[axis]."""
+    freqs, axes = [], []
+    for axis, n in enumerate(pairs_per_axis):
+        freqs += [float(theta) ** (-i / n) for i in range(n)]
+        axes += [axis] * n
+    return freqs, axes
+
+
+def dig_rope(q, k, positions, freqs, axes, *, interleaved=False, inverse=False, inplace=False):
+    """Turns pair i of every head's channels by positions[..., axes[i]] * freqs[i]; returns (q_out, k_out), k may be None.
+
+    q: [B, L, H, d]; k: [B, L, H_k, d], the last two dimensions dense; positions: int32 [L, axes] or [B, L, axes].  Pairs are channels
+    (i, i + n), or (2i, 2i + 1) with `interleaved`; `inverse` turns back (the gradient); `inplace` writes to q and k."""
+    return _binding().rope(q, k, positions, freqs, axes, interleaved, inverse, inplace)
+
+
+def dig_layernorm_fwd(x, w=None, b=None, eps=1e-5):
+    """Layer norm over the last axis of x; w, b: fp32 [D], or [groups, D] for as many groups of consecutive rows, or None."""
+    return _binding().layernorm_fwd(x, w, b, eps)
+
+
+def dig_layernorm_bwd(x, dy, w=None, eps=1e-5, *, affine_grads=True, workspace=None):
+    """Returns (dx, dw, db); the last two are fp32 of w's shape ([D] where it is None), or None without `affine_grads`."""
+    return _binding().layernorm_bwd(x, dy, w, eps, affine_grads, workspace)
