@@ -75,7 +75,8 @@ dig_status launch_share_sum(const float *part, void *out, long long rows, int H,
 
 // Rows of a tile, and the two kinds of kernels.
 constexpr int kTileFma = 64, kTileTc = 128;
-dig_status fma_pass(const Args &a, bool local, int dtype, cudaStream_t stream);
+dig_status fma_pass(const Args &a, bool local, cudaStream_t stream);         // fp32 storage
+dig_status tc_pass(const Args &a, bool local, cudaStream_t stream);          // bf16 storage
 
 }  // namespace decay
 }  // namespace dig

@@ -9,10 +9,9 @@ namespace {
 constexpr int T = kTileFma, NT = 256, LDP = T + 4;
 
 // Rows of a tile as fp32 in shared memory, stride d + 4 floats (a step of one row is a step of 4 banks); rows behind the end zero.
-template <typename S>
 __device__ __forceinline__ void load_rows(float *dst, const Args &a, const Rows &r, int d, int dir, int b, int h, int p0, int n)
 {
-    const S *base = (const S *)r.p + (size_t)b * r.batch + (size_t)(h / r.share) * d;
+    const float *base = (const float *)r.p + (size_t)b * r.batch + (size_t)(h / r.share) * d;
     for (int i = threadIdx.x; i < T * (d / 4); i += NT) {
         const int row = i / (d / 4), c = (i - row * (d / 4)) * 4, p = p0 + row;
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -28,7 +27,7 @@ __device__ __forceinline__ void axpy4(float4 &s, float w, float4 x)
 }
 __device__ __forceinline__ float4 scaled(float4 x, float w) { return make_float4(x.x * w, x.y * w, x.z * w, x.w * w); }
 
-template <typename S, bool LOCAL>
+template <bool LOCAL>
 __global__ void __launch_bounds__(NT) decay_fma(const __grid_constant__ Args a)
 {
     extern __shared__ float4 smem4[];
@@ -54,9 +53,9 @@ __global__ void __launch_bounds__(NT) decay_fma(const __grid_constant__ Args a)
         const int p0 = t * T, rows = min(T, n - p0), lead = p0 == 0 ? ps.first : 1;
         __syncthreads();
         if (rows > 0) {
-            load_rows<S>(K, a, ps.k, dk, ps.dir, b, h, p0, n);
-            load_rows<S>(V, a, ps.v, dv, ps.dir, b, h, p0, n);
-            if (!LOCAL) load_rows<S>(Q, a, ps.q, dk, ps.dir, b, h, p0, n);
+            load_rows(K, a, ps.k, dk, ps.dir, b, h, p0, n);
+            load_rows(V, a, ps.v, dv, ps.dir, b, h, p0, n);
+            if (!LOCAL) load_rows(Q, a, ps.q, dk, ps.dir, b, h, p0, n);
         }
         __syncthreads();
         if (!LOCAL) {
@@ -106,8 +105,7 @@ __global__ void __launch_bounds__(NT) decay_fma(const __grid_constant__ Args a)
                     if (p < n) axpy4(o[i], pw[r] * (lead ? pw[1] : 1.f), e[i]);
                     const size_t at = ((size_t)b * a.L + token_at(a, ps.dir, p, n)) * tok + (size_t)h * dv + c;
                     const float4 y = p < n ? o[i] : make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (ps.out_f32) store4((float *)ps.out + at, y);
-                    else store4((S *)ps.out + at, y);
+                    store4((float *)ps.out + at, y);
                 }
             }
             __syncthreads();
@@ -144,25 +142,21 @@ size_t smem_bytes(int dk, int dv, bool local)
     return f * 4;
 }
 
-template <typename S, bool LOCAL>
+template <bool LOCAL>
 dig_status launch(const Args &a, cudaStream_t stream)
 {
     int segs = a.nseg;
     size_t smem = 0;
     for (int i = 0; i < a.passes; ++i) smem = smem > smem_bytes(a.pass[i].dk, a.pass[i].dv, LOCAL) ? smem : smem_bytes(a.pass[i].dk, a.pass[i].dv, LOCAL);
-    dig_status st = ensure_dynamic_smem((const void *)decay_fma<S, LOCAL>, smem);
+    dig_status st = ensure_dynamic_smem((const void *)decay_fma<LOCAL>, smem);
     if (st != DIG_OK) return st;
     KernelTimer t(LOCAL ? KID_DECAY_LOCAL : KID_DECAY, stream);
-    return cuda_ok(launch_pdl(decay_fma<S, LOCAL>, dim3(segs, a.B * a.H, a.passes), dim3(NT), smem, stream, a));
+    return cuda_ok(launch_pdl(decay_fma<LOCAL>, dim3(segs, a.B * a.H, a.passes), dim3(NT), smem, stream, a));
 }
 
 }  // namespace
 
-dig_status fma_pass(const Args &a, bool local, int dtype, cudaStream_t stream)
-{
-    if (dtype == DIG_F32) return local ? launch<float, true>(a, stream) : launch<float, false>(a, stream);
-    return local ? launch<__nv_bfloat16, true>(a, stream) : launch<__nv_bfloat16, false>(a, stream);
-}
+dig_status fma_pass(const Args &a, bool local, cudaStream_t stream) { return local ? launch<true>(a, stream) : launch<false>(a, stream); }
 
 }  // namespace decay
 }  // namespace dig

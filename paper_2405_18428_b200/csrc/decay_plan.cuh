@@ -29,16 +29,15 @@ struct Plan {
     int tile, nseg, G;
 };
 // One CTA per sequence and pass where that fills the machine; else as many segments as give every SM its CTAs.
-inline Plan make_plan(int B, int H, int L, int passes, int dtype)
+inline Plan make_plan(int B, int H, int L, int passes, int d, int dtype)
 {
     Plan p;
-    p.tile = kTileFma;
-    const long long tiles = (L + p.tile - 1) / p.tile, seqs = (long long)B * H * passes, room = 2ll * kSms;
+    p.tile = dtype == DIG_F32 ? kTileFma : kTileTc;
+    const long long tiles = (L + p.tile - 1) / p.tile, seqs = (long long)B * H * passes, room = (dtype == DIG_BF16 && d > 80 ? 1ll : 2ll) * kSms;
     long long nseg = seqs * 2 > room ? 1 : room / seqs;
     if (nseg > tiles) nseg = tiles;
     p.G = (int)((tiles + nseg - 1) / nseg);
     p.nseg = (int)((tiles + p.G - 1) / p.G);
-    (void)dtype;
     return p;
 }
 
@@ -52,7 +51,7 @@ struct Carved {
 inline Carved carve(char *base, int B, int H, int H_kv, int L, int dk, int dv, int dtype, bool backward)
 {
     Carved w{};
-    w.plan = make_plan(B, H, L, backward ? 3 : 1, dtype);
+    w.plan = make_plan(B, H, L, backward ? 3 : 1, dk > dv ? dk : dv, dtype);
     size_t o = 0;
     auto take = [&](size_t bytes) { char *p = base + o; o += align256(bytes); return reinterpret_cast<float *>(p); };
     const size_t state = w.plan.nseg > 1 ? (size_t)B * H * w.plan.nseg * dk * dv * 4 : 16;
@@ -81,7 +80,7 @@ inline bool set_decay(Log2Decay &l, const float *log_decay, int H)
 
 inline dig_status pass_kernel(const Args &a, bool local, int dtype, cudaStream_t stream)
 {
-    return fma_pass(a, local, dtype, stream);
+    return dtype == DIG_F32 ? fma_pass(a, local, stream) : tc_pass(a, local, stream);
 }
 
 }  // namespace decay
