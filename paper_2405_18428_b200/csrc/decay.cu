@@ -6,10 +6,10 @@ namespace dig {
 namespace decay {
 namespace {
 
-// State entering every segment of a sequence, in place of the segment's own contribution, and the state behind the last one.  A thread
-// has one element of the state; the loads of a group of segments do not depend on one another.
+// Joins the segments of a sequence: the state entering every one, in place of the segment's own contribution, or (x_end) the state
+// behind the last.  A thread has one element of the state; the loads of a group of segments do not depend on one another.
 struct ScanArgs {
-    Pass pass[2];
+    Pass pass[kMaxPasses];
     int H, L, nseg, span;                // span: positions of a segment
     const int *lengths;
     Log2Decay lam;
@@ -36,11 +36,11 @@ __global__ void __launch_bounds__(256) decay_scan(const __grid_constant__ ScanAr
         for (int i = 0; i < kGroup; ++i) {
             const int s = s0 + i, rows = min(max(n - s * a.span, 0), a.span);
             if (s >= a.nseg) break;
-            u[(size_t)s * dd] = x;
+            if (!ps.x_end) u[(size_t)s * dd] = x;
             if (rows > 0) x = fmaf(exp2_of(lam * (rows - (s == 0 ? 1 - ps.first : 0))), x, own[i]);
         }
     }
-    if (ps.x_end) ps.x_end[(size_t)bh * dd + e] = n > 0 && ps.last ? x * exp2_of(lam) : x;
+    if (ps.x_end) ps.x_end[(size_t)bh * dd + e] = n > 0 && ps.last ? x * exp2_of(lam) : x;         // no token: the start state
 }
 
 // out[t][hk] = sum over the heads that share hk, in their order.
@@ -64,18 +64,18 @@ __global__ void __launch_bounds__(256) share_sum(const float *__restrict__ part,
 
 }  // namespace
 
-dig_status launch_scan(const Args &a, int tile, const int *which, int n, cudaStream_t stream)
+dig_status launch_scan(const Args &a, int tile, cudaStream_t stream)
 {
     ScanArgs s;
     int most = 0;
-    for (int i = 0; i < n; ++i) {
-        s.pass[i] = a.pass[which[i]];
+    for (int i = 0; i < a.passes; ++i) {
+        s.pass[i] = a.pass[i];
         const int dd = s.pass[i].dk * s.pass[i].dv;
         most = dd > most ? dd : most;
     }
     s.H = a.H; s.L = a.L; s.nseg = a.nseg; s.span = a.G * tile; s.lengths = a.lengths; s.lam = a.lam;
     KernelTimer t(KID_DECAY_SCAN, stream);
-    return cuda_ok(launch_pdl(decay_scan, dim3((most + 255) / 256, a.B * a.H, n), dim3(256), 0, stream, s));
+    return cuda_ok(launch_pdl(decay_scan, dim3((most + 255) / 256, a.B * a.H, a.passes), dim3(256), 0, stream, s));
 }
 
 dig_status launch_share_sum(const float *part, void *out, long long rows, int H, int share, int d, int dtype, cudaStream_t stream)
@@ -169,16 +169,21 @@ Rows rows_of(const void *p, const long long *strides, long long L, int heads, in
     return r;
 }
 
-// Local pass and scan where the sequences are cut, then the pass itself.  `which`: the passes that have a state of their own.
-dig_status run(Args &a, const Plan &pl, const int *which, int n, int dtype, cudaStream_t stream)
+// Local pass and scan for the states that enter segments, where the sequences are cut (of the passes that have states of their own, the
+// first `n`), and for the state that the caller wants (of the pass `end`), then the passes themselves.
+dig_status run(Args &a, const Carved &w, int n, int end, int dtype, cudaStream_t stream)
 {
-    a.nseg = pl.nseg; a.G = pl.G;
-    if (pl.nseg > 1) {
-        Args l = a;
-        for (int i = 0; i < n; ++i) l.pass[i] = a.pass[which[i]];
-        l.passes = n;
+    a.nseg = w.plan.nseg; a.G = w.plan.G;
+    Args l = a;
+    l.passes = a.nseg > 1 ? n : 0;
+    for (int i = 0; i < l.passes; ++i) l.pass[i].x_end = nullptr;
+    if (a.pass[end].x_end) {
+        l.pass[l.passes] = a.pass[end];
+        l.pass[l.passes++].local = w.final;
+    }
+    if (l.passes > 0) {
         dig_status st = pass_kernel(l, true, dtype, stream);
-        if (st == DIG_OK) st = launch_scan(a, pl.tile, which, n, stream);
+        if (st == DIG_OK) st = launch_scan(l, w.plan.tile, stream);
         if (st != DIG_OK) return st;
     }
     return pass_kernel(a, false, dtype, stream);
@@ -193,14 +198,14 @@ dig_status decay_fwd_launch(const DecayCall &c)
     Args a{};
     if (!set_decay(a.lam, c.log_decay, c.H)) return DIG_ERR_INVALID_ARG;
     a.passes = 1; a.B = c.B; a.H = c.H; a.L = c.L; a.gh = c.gh; a.gw = c.gw; a.lengths = c.lengths;
+    a.gh_inv = c.gh == 1 ? 0xffffffffu : (uint32_t)((1ull << 32) / c.gh);
     Pass &p = a.pass[0];
     p.q = rows_of(c.q, c.strides, c.L, c.H, c.dk, 1);
     p.k = rows_of(c.k, c.strides ? c.strides + 2 : nullptr, c.L, c.H_kv, c.dk, share);
     p.v = rows_of(c.v, c.strides ? c.strides + 4 : nullptr, c.L, c.H_kv, c.dv, share);
     p.out = c.out; p.x0 = c.s_in; p.local = w.local[0]; p.x_end = c.s_out;
     p.dk = c.dk; p.dv = c.dv; p.dir = c.dir; p.first = 1; p.last = 0;
-    const int which[1] = {0};
-    return run(a, w.plan, which, 1, c.dtype, c.stream);
+    return run(a, w, 1, 0, c.dtype, c.stream);
 }
 
 dig_status decay_bwd_launch(const DecayCall &c)
@@ -210,6 +215,7 @@ dig_status decay_bwd_launch(const DecayCall &c)
     Args a{};
     if (!set_decay(a.lam, c.log_decay, c.H)) return DIG_ERR_INVALID_ARG;
     a.passes = 3; a.B = c.B; a.H = c.H; a.L = c.L; a.gh = c.gh; a.gw = c.gw; a.lengths = c.lengths;
+    a.gh_inv = c.gh == 1 ? 0xffffffffu : (uint32_t)((1ull << 32) / c.gh);
     const Rows q = rows_of(c.q, c.strides, c.L, c.H, c.dk, 1), k = rows_of(c.k, c.strides ? c.strides + 2 : nullptr, c.L, c.H_kv, c.dk, share),
                v = rows_of(c.v, c.strides ? c.strides + 4 : nullptr, c.L, c.H_kv, c.dv, share), g = rows_of(c.d_out, nullptr, c.L, c.H, c.dv, 1);
     Pass &dq = a.pass[0], &dv = a.pass[1], &dk = a.pass[2];
@@ -219,8 +225,7 @@ dig_status decay_bwd_launch(const DecayCall &c)
     dv.dk = c.dk; dv.dv = c.dv; dv.dir = c.dir ^ 1; dv.last = 1; dv.out_f32 = share > 1;
     dk.q = v; dk.k = g; dk.v = q; dk.out = share > 1 ? (void *)w.part_k : c.dk_out; dk.x0 = c.ds_out; dk.x_transposed = 1; dk.local = w.local[1];
     dk.local_transposed = 1; dk.dk = c.dv; dk.dv = c.dk; dk.dir = c.dir ^ 1; dk.out_f32 = share > 1;
-    const int which[2] = {0, 1};
-    dig_status st = run(a, w.plan, which, 2, c.dtype, c.stream);
+    dig_status st = run(a, w, 2, 1, c.dtype, c.stream);
     if (st != DIG_OK || share == 1) return st;
     st = launch_share_sum(w.part_k, c.dk_out, (long long)c.B * c.L, c.H, share, c.dk, c.dtype, c.stream);
     return st != DIG_OK ? st : launch_share_sum(w.part_v, c.dv_out, (long long)c.B * c.L, c.H, share, c.dv, c.dtype, c.stream);

@@ -40,7 +40,7 @@ struct Pass {
     void *out;
     const float *x0;
     float *local;
-    float *x_end;                        // where wanted: g^last (state behind the last position)
+    float *x_end;                        // where wanted: g^last (state behind the last position); in the scan alone
     int dk, dv, dir, first, last, x_transposed, local_transposed, out_f32;
 };
 
@@ -48,6 +48,7 @@ struct Args {
     Pass pass[kMaxPasses];
     int passes, B, H, L, gh, gw, nseg, G;         // G: tiles of a segment
     const int *lengths;                  // [B] or null
+    uint32_t gh_inv;                     // floor(2^32 / gh), 2^32 - 1 for one row: column orders divide by the grid's height
     Log2Decay lam;
 };
 
@@ -69,7 +70,7 @@ __device__ __forceinline__ float exp2_of(float x)
 }
 
 // Joins segments: kernel of decay_scan.cu.
-dig_status launch_scan(const Args &a, int tile, const int *which, int n, cudaStream_t stream);
+dig_status launch_scan(const Args &a, int tile, cudaStream_t stream);
 // Sums the partial gradients of heads that share keys and values.
 dig_status launch_share_sum(const float *part, void *out, long long rows, int H, int share, int d, int dtype, cudaStream_t stream);
 

@@ -30,6 +30,11 @@ __device__ __forceinline__ float4 scaled(float4 x, float w) { return make_float4
 template <bool LOCAL>
 __global__ void __launch_bounds__(NT) decay_fma(const __grid_constant__ Args a)
 {
+    if (LOCAL && blockIdx.x == a.nseg - 1 && !a.pass[blockIdx.z].x_end) {            // goes into the final state only
+        pdl_wait();
+        pdl_launch_dependents();
+        return;
+    }
     extern __shared__ float4 smem4[];
     float *sm = reinterpret_cast<float *>(smem4);
     const Pass &ps = a.pass[blockIdx.z];
@@ -129,9 +134,6 @@ __global__ void __launch_bounds__(NT) decay_fma(const __grid_constant__ Args a)
     __syncthreads();
     if (LOCAL) {
         for (int i = tid; i < dk * dv; i += NT) local[i] = X[i / dv * ldv + i % dv];
-    } else if (ps.x_end && a.nseg == 1) {
-        const float f = n > 0 && ps.last ? pw[1] : 1.f;          // no token: the start state
-        for (int i = tid; i < dk * dv; i += NT) ps.x_end[(size_t)bh * dd + i] = X[i / dv * ldv + i % dv] * f;
     }
     pdl_launch_dependents();
 }

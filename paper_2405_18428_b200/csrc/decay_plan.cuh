@@ -28,24 +28,37 @@ namespace decay {
 struct Plan {
     int tile, nseg, G;
 };
-// One CTA per sequence and pass where that fills the machine; else as many segments as give every SM its CTAs.
+// How many segments: time in tiles of the pass, a round of segments on all SMs at a time, plus the local pass (two CTAs on an SM, half a
+// tile's time each) and its launches where there is a cut.
 inline Plan make_plan(int B, int H, int L, int passes, int d, int dtype)
 {
     Plan p;
     p.tile = dtype == DIG_F32 ? kTileFma : kTileTc;
-    const long long tiles = (L + p.tile - 1) / p.tile, seqs = (long long)B * H * passes, room = (dtype == DIG_BF16 && d > 80 ? 1ll : 2ll) * kSms;
-    long long nseg = seqs * 2 > room ? 1 : room / seqs;
-    if (nseg > tiles) nseg = tiles;
-    p.G = (int)((tiles + nseg - 1) / nseg);
-    p.nseg = (int)((tiles + p.G - 1) / p.G);
+    const long long tiles = (L + p.tile - 1) / p.tile, seqs = (long long)B * H * passes, sms = (dtype == DIG_F32 ? 2 : 1) * kSms;
+    auto ceil_div = [](long long x, long long y) { return (x + y - 1) / y; };
+    double least = 0;
+    p.nseg = 0;
+    for (long long want = 1; want <= tiles && want <= kSms; ++want) {
+        const long long G = ceil_div(tiles, want), nseg = ceil_div(tiles, G);
+        if (nseg != want) continue;
+        double t = ceil_div(seqs * nseg, sms) * (G + 1.0);
+        if (nseg > 1) t += ceil_div(seqs * nseg, sms * 2) * (G + 1.0) + 2.0;
+        if (p.nseg == 0 || t < least) {
+            least = t;
+            p.nseg = (int)nseg;
+            p.G = (int)G;
+        }
+        if (seqs * nseg >= 2 * sms) break;
+    }
+    (void)d;
     return p;
 }
 
-// Workspace, every block 256-byte aligned: states of the segments, [B*H][nseg][dk][dv] fp32 (backward: twice), and where heads share
-// keys and values the gradients of each head before they are summed, fp32 [B][L][H][d].
+// Workspace, every block 256-byte aligned: states of the segments, [B*H][nseg][dk][dv] fp32 (backward: of two passes), the same once
+// more for the final state, and where heads share keys and values the gradients of each head before they are summed, fp32 [B][L][H][d].
 struct Carved {
     Plan plan;
-    float *local[2], *part_k, *part_v;
+    float *local[2], *final, *part_k, *part_v;
     size_t bytes;
 };
 inline Carved carve(char *base, int B, int H, int H_kv, int L, int dk, int dv, int dtype, bool backward)
@@ -56,6 +69,7 @@ inline Carved carve(char *base, int B, int H, int H_kv, int L, int dk, int dv, i
     auto take = [&](size_t bytes) { char *p = base + o; o += align256(bytes); return reinterpret_cast<float *>(p); };
     const size_t state = w.plan.nseg > 1 ? (size_t)B * H * w.plan.nseg * dk * dv * 4 : 16;
     w.local[0] = take(state);
+    w.final = take((size_t)B * H * w.plan.nseg * dk * dv * 4);
     if (backward) {
         w.local[1] = take(state);
         if (H != H_kv) {

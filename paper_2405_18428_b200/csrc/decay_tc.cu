@@ -1,17 +1,24 @@
 // Linear attention with a decay for each head on the tcgen05 tensor cores (equations in decay.cuh): bf16 storage, heads of up to
-// 128 channels.  A CTA walks over the 128-position tiles of a segment with the state in registers.
+// 128 channels.
 //
-// The decay is a number per head, so q, k and v are operands as they come: a tile is copied to shared memory (cp.async, 16 bytes a
-// thread, any row strides and scan order), S = Q K^T and I = Q X go to tensor memory, threads weigh the scores, P = S . g^(i-j), and
-// leave them there as the bf16 A operand of O = P V, and the state takes U = (g^(n-1-j) k_j)^T v_j: X' = g^n X + U.
-// Powers are at most 1 everywhere; only within the diagonal blocks of 16 keys they are formed one by one, elsewhere as
-// g^(i-j0-15) g^(15-(j-j0)), the second factor the same for all rows.
+// The decay is a number per head, so q, k and v are operands as they come: a tile of 128 positions is copied to shared memory, S = Q K^T
+// and I = Q X go to tensor memory, threads weigh the scores, P = S . g^(i-j), and leave them there as the bf16 A operand of O = P V,
+// and the state takes U = (g^(n-1-j) k_j)^T v_j: X' = g^n X + U.  Powers are at most 1 everywhere; only within the diagonal blocks of 32
+// keys they are formed one by one, elsewhere as g^(i-j0-15) g^(15-(j-j0)), the second factor the same for all rows.
 //
-// Roundings to bf16: P, the state where it is an operand, the decayed keys; each 2^-9 of its term on average, as much as the rounding of
-// the results.  A state that the caller gets has its decayed keys in two bf16 parts (2^-16).
+// Roundings to bf16: P and the decayed keys, each 2^-9 of its term on average, as much as the rounding of the results; the state
+// is an operand in two bf16 parts.  A state that the caller gets is summed apart, with its decayed keys in three bf16 parts (2^-24).
 //
-// Tile layout: chunk-major without swizzle, element (row, col) at (col / 8) * (16 R + 16) + 16 row + 2 (col % 8): both operand orientations
-// from the same bytes, heads of any multiple of 8, no bank conflicts for rows or columns of 16 bytes.
+// One CTA per SM works through a list of segments; its warps have parts of their own, so that the loads of one tile, the scores of the
+// next, the state of this one and the results of the one before overlap:
+//   warps 0 .. 7    scores to decayed scores
+//   warps 8 .. 15   decayed keys, state
+//   warps 16 .. 19  results
+//   warps 20 .. 22  loads of q, k, v;  warp 23  products
+// Five parts on every scheduler share its instruction cache: loops are kept short and rolled, and what is rare stands apart.  Unrolled, two
+// thirds of the warps' time went by waiting for instructions (4 x 4096 tokens of 12 heads of 64 channels: 60 us).
+#include <type_traits>
+
 #include "decay_plan.cuh"
 #include "umma.cuh"
 
@@ -22,27 +29,52 @@ namespace {
 using namespace umma;
 using bf16 = __nv_bfloat16;
 
-constexpr int T = kTileTc, NT = 256, CH = T * 16 + 16;
+constexpr int T = kTileTc, CH = T * 16 + 16;
+constexpr int kScore = 8, kState = 8, kOut = 4, kLoad = kScore + kState + kOut, kMma = kLoad + 3, kThreads = (kMma + 1) * 32;
 
+// Layouts in shared memory.  q, k, v: panels of 64 channels, rows of 128 bytes under the 128-byte swizzle (a copy of eight lanes then
+// writes one line; chunk by chunk of 16 bytes apart it took four times as long), and where 64 or 128 do not hold the head, 16 channels
+// more in two chunks.  Decayed keys, state and results: chunk-major without swizzle, element (row, col) of R rows at
+// (col / 8) * (16 R + 16) + 16 row + 2 (col % 8).
 // D: channels that tiles provide for keys and values, the smallest of 64, 80 and 128 that holds both.
 template <int D>
 struct Cfg {
-    static constexpr int NCH = D / 8, KS = D / 16, TILE = NCH * CH, CHX = D * 16 + 16, XT = NCH * CHX;
+    static constexpr int PANELS = D / 64, REST = D % 64 / 16, TILE = PANELS * T * 128 + (REST ? 2 * CH + 992 : 0);
+    static constexpr int NCH = D / 8, CHX = D * 16 + 16, XT = NCH * CHX, KEYS = NCH * CH;
+    static constexpr int STAGES = D == 128 ? 1 : 2, KEY_BUFS = STAGES, S_BUFS = STAGES;      // what shared and tensor memory hold
     static constexpr int HALF = D / 2;                       // columns of a thread
-    // tensor memory: scores 0 .. 127, over them the decayed scores of keys 0 .. 63 (0 .. 31) and O; those of keys 64 .. 127 last
-    static constexpr int S = 0, P0 = 0, O = 64, I = O + D < 128 ? 128 : O + D, P1 = I + D, COLS = P1 + 32 <= 256 ? 256 : 512;
+    // tensor memory: scores (over them the decayed ones), outputs, what the entering state gives, the tile's own state
+    static constexpr int S = 0, O = S_BUFS * 128, I = O + D, U = I + D;
+    // shared memory: tiles, decayed keys, state (two parts), results
+    static constexpr int Q = 0, K = STAGES * TILE, V = 2 * STAGES * TILE, KD = 3 * STAGES * TILE, X = KD + KEY_BUFS * KEYS, R = X + 2 * XT;
+    static constexpr int BYTES = R + KEYS + 1024;
+    // a product reads sixteen chunks of decayed keys from where they start
+    static_assert(TILE % 1024 == 0 && U + D <= 512 && KD + (KEY_BUFS - 1) * KEYS + 16 * CH <= BYTES - 1024 && BYTES + 768 <= 227 * 1024, "fits");
 };
+// Column of the decayed scores of keys 16 kk ..: the warps of keys 0 .. 31 and 64 .. 95 write over scores they have read themselves, and
+// so do those of the others.
+__device__ __forceinline__ constexpr int p_col(int kk) { return (kk >> 2) * 16 + (kk >> 1 & 1) * 32 + (kk & 1) * 8; }
 
-struct Ctl {
-    uint64_t bar[2];
+// Barriers: two of each, tile i of the CTA's list uses i & 1 in phase i >> 1.  Nobody may be two phases behind on one: each is completed
+// again only after all that wait for it have gone on.
+struct Bars {
+    uint64_t q[2], k[2], v[2];           // loaded
+    uint64_t s[2], i[2], u[2], o[2];     // products done: scores; scores and what the state gives; the tile's state; outputs
+    uint64_t p[2], kd[2], x[2];          // written: decayed scores, decayed keys, state
+    uint64_t uf[2], of[2];               // read: the tile's state; outputs and what the state gives
     uint32_t tmem;
     int dead;                            // a wait gave up: no more waiting
-    int tok[2][T];
+};
+struct Ctl : Bars {
+    int tok[T];                          // token of every row of the tile whose results are on their way
 };
 
 __host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, bool a_mn, bool b_mn) { return idesc_f16(M, N, a_mn, b_mn) | (1u << 7) | (1u << 10); }
 __device__ __forceinline__ uint64_t kmajor(uint32_t a, uint32_t ch) { return make_desc(a, ch, 128, 0); }
 __device__ __forceinline__ uint64_t mnmajor(uint32_t a, uint32_t ch) { return make_desc(a, 128, ch, 0); }
+// Panels: groups of 8 rows are 1024 bytes apart; along the channels, the next panel.
+__device__ __forceinline__ uint64_t kmajor_panel(uint32_t a) { return make_desc(a, 16, 1024, 2); }
+__device__ __forceinline__ uint64_t mnmajor_panel(uint32_t a) { return make_desc(a, T * 128, 1024, 2); }
 
 // A from tensor memory.  Lanes of the quarters below `skip` keep what they hold.
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate, int skip)
@@ -83,399 +115,676 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void *src, int bytes)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void copy_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" :: "n"(N) : "memory"); }
-
+// Until this thread's copies have arrived; then they are there for the tensor core too.
+__device__ __forceinline__ void copies_done()
+{
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    fence_async_smem();
+}
+__device__ __forceinline__ void arrive(uint64_t *bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(smem_u32(bar)) : "memory"); }
+// A warp's writes to shared or tensor memory are done.
+__device__ __forceinline__ void warp_arrive(uint64_t *bar)
+{
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) arrive(bar);
+}
+__device__ __forceinline__ void sync_out_warps() { asm volatile("bar.sync 1, %0;" :: "n"(kOut * 32) : "memory"); }
 __device__ __forceinline__ void zero16(char *p) { *reinterpret_cast<uint4 *>(p) = make_uint4(0, 0, 0, 0); }
 
-// The rows of one operand for this CTA's sequence and head.
-struct Src {
-    const bf16 *p;
-    long long token;
-    int nch;                             // chunks of 8 channels
-};
-__device__ __forceinline__ Src src_of(const Rows &r, int b, int h, int d)
+__device__ __forceinline__ bool passed(uint64_t *bar, uint32_t parity)
 {
-    return {(const bf16 *)r.p + (size_t)b * r.batch + (size_t)(h / r.share) * d, r.token, d / 8};
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(smem_u32(bar)), "r"(parity) : "memory");
+    return ok;
 }
-// A tile's rows; consecutive threads take the chunks of a row.
-__device__ __forceinline__ void load_tile(uint32_t dst, const Src &s, const int *tok)
-{
-    const uint32_t inv = (0xffffffffu / s.nch) + 1;          // exact for dividends below 2^16, but 2^32 does not fit: one chunk apart
-    for (uint32_t i = threadIdx.x; i < (uint32_t)(T * s.nch); i += NT) {
-        const uint32_t row = s.nch == 1 ? i : __umulhi(i, inv), c = i - row * s.nch;
-        const int t = tok[row];
-        copy16(dst + c * CH + row * 16, s.p + (size_t)max(t, 0) * s.token + c * 8, t >= 0 ? 16 : 0);
-    }
-}
-// Token of every row of a tile, -1 behind the end.
-__device__ __forceinline__ void tokens(int *tok, const Args &a, int dir, int tile, int n)
-{
-    if (threadIdx.x < T) {
-        const int p = tile * T + threadIdx.x;
-        tok[threadIdx.x] = p < n ? scan_token(p, dir, a.gh, a.gw, n) : -1;
-    }
-}
-// Decayed keys, hi + lo: row j times g^(last - j).  Thread: one row, every second chunk.
-__device__ __forceinline__ void decay_keys(const char *K, char *hi, char *lo, int nch, float lam, int last, bool exact)
-{
-    const int j = threadIdx.x & (T - 1);
-    const float w = exp2_of(lam * max(last - j, 0));
-    for (int c = threadIdx.x / T; c < nch; c += NT / T) {
-        const uint4 u = *reinterpret_cast<const uint4 *>(K + c * CH + j * 16);
-        uint32_t x[4] = {u.x, u.y, u.z, u.w}, y[4], z[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float p = lo_f(x[i]) * w, q = hi_f(x[i]) * w;
-            y[i] = pack(p, q);
-            z[i] = pack(p - lo_f(y[i]), q - hi_f(y[i]));
-        }
-        *reinterpret_cast<uint4 *>(hi + c * CH + j * 16) = make_uint4(y[0], y[1], y[2], y[3]);
-        if (exact) *reinterpret_cast<uint4 *>(lo + c * CH + j * 16) = make_uint4(z[0], z[1], z[2], z[3]);
-    }
-}
-__device__ __forceinline__ void wait(Ctl *ctl, int which, uint32_t parity, int *status)
+__device__ __noinline__ void wait_on(Bars *ctl, uint64_t *bar, uint32_t parity, int *status)
 {
     if (*(volatile int *)&ctl->dead) return;
-    if (!mbar_wait(&ctl->bar[which], parity, status)) *(volatile int *)&ctl->dead = 1;
+    if (!mbar_wait(bar, parity, status)) *(volatile int *)&ctl->dead = 1;
 }
-// U (+)= KT^T V: M = 128, rows beyond the keys' channels are whatever follows in shared memory and are not used.
-template <int D>
-__device__ __forceinline__ void issue_state(uint32_t d, uint32_t kt, uint32_t v, bool accumulate)
+// Waits for tile i's phase of a pair of barriers.
+__device__ __forceinline__ void wait(Bars *ctl, uint64_t *pair, int i, int *status)
 {
-    const uint64_t a = mnmajor(kt, CH), b = mnmajor(v, CH);
-#pragma unroll
-    for (int kk = 0; kk < T / 16; ++kk) mma_f16(d, a + kk * 16, b + kk * 16, idesc_bf16(128, D, true, true), accumulate || kk > 0);
+    if (!passed(pair + (i & 1), i >> 1 & 1)) wait_on(ctl, pair + (i & 1), i >> 1 & 1, status);
+    __syncwarp();
+}
+__device__ __forceinline__ bool ready(uint64_t *pair, int i)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(ok) : "r"(smem_u32(pair + (i & 1))), "r"(i >> 1 & 1) : "memory");
+    return __all_sync(0xffffffffu, ok);
 }
 
-// Rows of results: 8 columns of one.
-__device__ __forceinline__ void put8(const Pass &ps, size_t at, const float (&o)[8])
+// One segment of one sequence and pass.
+struct Item {
+    int pass, seg, b, h, n, t0, t1, t_end;       // n: tokens of the sequence; t_end: behind the last tile that has any
+};
+__device__ __forceinline__ Item item_at(const Args &a, int i)
 {
-    if (ps.out_f32) {
-        float *p = (float *)ps.out + at;
-        store4(p, make_float4(o[0], o[1], o[2], o[3]));
-        store4(p + 4, make_float4(o[4], o[5], o[6], o[7]));
-    } else {
-        *reinterpret_cast<uint4 *>((bf16 *)ps.out + at) = make_uint4(pack(o[0], o[1]), pack(o[2], o[3]), pack(o[4], o[5]), pack(o[6], o[7]));
+    Item w;
+    w.pass = i % a.passes; i /= a.passes;
+    w.seg = i % a.nseg; i /= a.nseg;
+    w.b = i / a.H; w.h = i - w.b * a.H;
+    w.n = length_of(a.lengths, a.L, w.b);
+    w.t0 = w.seg * a.G;
+    w.t1 = min(w.t0 + a.G, (a.L + T - 1) / T);
+    w.t_end = min(w.t1, (w.n + T - 1) / T);
+    return w;
+}
+
+// ---- the loading warps --------------------------------------------------------------------------------------------------
+// Token at a position before the end; behind it, ~position.
+__device__ __forceinline__ int token_or_not(const Args &a, int dir, int p, int n)
+{
+    int q = dir & 1 ? n - 1 - p : p;
+    if (dir & 2) {
+        // q / gh with a reciprocal rounded down: the estimate is at most one too small for q < 2^24
+        int x = (int)__umulhi((uint32_t)q, a.gh_inv), y = q - x * a.gh;
+        if (y >= a.gh) { y -= a.gh; ++x; }
+        q = y * a.gw + x;
     }
+    return p < n ? q : ~p;
 }
-
+// Rows of one operand for a sequence and head, 32 at a time: panels, eight lanes to a row's 128 bytes, and the rest.
 template <int D>
-__global__ void __launch_bounds__(NT, D <= 80 ? 2 : 1) decay_pass(const __grid_constant__ Args a, int *status)
+__device__ __forceinline__ void load_tile(const Args &a, uint32_t dst, const Rows &r, const Item &w, int dir, int tile, int d)
 {
     using C = Cfg<D>;
-    extern __shared__ __align__(128) char sm[];
-    __shared__ Ctl ctl;
-    const Pass &ps = a.pass[blockIdx.x % a.passes];
-    const int seg = blockIdx.x / a.passes, bh = blockIdx.y, b = bh / a.H, h = bh - b * a.H, dk = ps.dk, dv = ps.dv;
-    const float lam = a.lam.v[h];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;
-    const bool exact = true, ends = ps.x_end && a.nseg == 1;
-    // decayed keys first: their products read sixteen chunks from their start
-    char *KH = sm, *KL = KH + dk / 8 * CH, *Q = KL + (exact ? dk / 8 * CH : 0), *K = Q + C::TILE, *V = K + C::TILE, *X = V + C::TILE;
-    const uint32_t kh = smem_u32(KH), kl = smem_u32(KL), q = smem_u32(Q), k = smem_u32(K), v = smem_u32(V), x = smem_u32(X);
+    const bf16 *base = (const bf16 *)r.p + (size_t)w.b * r.batch + (size_t)(w.h / r.share) * d;
+    const int stride = (int)r.token, nch = d / 8, lane = threadIdx.x & 31, c0 = lane & 7, r0 = lane >> 3;
+    // rows r0, r0 + 4, ...: their low three bits alternate
+    const uint32_t even = r0 * 128 + ((c0 ^ r0) << 4), odd = (r0 + 4) * 128 + ((c0 ^ (r0 + 4)) << 4);
+#pragma unroll 1
+    for (int i = 0; i < T / 32; ++i) {
+        const int mine = token_or_not(a, dir, tile * T + i * 32 + lane, w.n);
+#pragma unroll 1
+        for (int panel = 0; panel < C::PANELS; ++panel) {
+            const int c = panel * 8 + c0;
+            const bf16 *p = base + c * 8;
+            const uint32_t to = dst + panel * T * 128 + i * 32 * 128;
+#pragma unroll
+            for (int m = 0; m < 8; ++m) {
+                const int t = __shfl_sync(0xffffffffu, mine, m * 4 + r0);
+                if (c < nch) copy16(to + (m & 1 ? odd : even) + (m & ~1) * 4 * 128, p + (long long)max(t, 0) * stride, t >= 0 ? 16 : 0);
+            }
+        }
+        if constexpr (C::REST > 0)
+            for (int c = C::PANELS * 8; c < nch; ++c)
+                copy16(dst + C::PANELS * T * 128 + (c - C::PANELS * 8) * CH + (i * 32 + lane) * 16, base + (long long)max(mine, 0) * stride + c * 8, mine >= 0 ? 16 : 0);
+    }
+}
+// Place of chunk c of row r in a tile.
+template <int D>
+__device__ __forceinline__ int chunk_at(int r, int c)
+{
+    using C = Cfg<D>;
+    return C::REST > 0 && c >= C::PANELS * 8 ? C::PANELS * T * 128 + (c - C::PANELS * 8) * CH + r * 16 : (c >> 3) * T * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+}
 
-    if (warp == 0) tmem_alloc(&ctl.tmem, C::COLS);
+// ---- products -----------------------------------------------------------------------------------------------------------
+// Over the channels of q, 16 at a time: go(step, descriptor of q, its offset from the tile's start in panels and steps of 32 bytes).
+template <int D, class F>
+__device__ __forceinline__ void each_channel_step(uint32_t tile, int ks, F go)
+{
+    using C = Cfg<D>;
+#pragma unroll 1
+    for (int kk = 0; kk < (C::REST > 0 ? min(ks, C::PANELS * 4) : ks); ++kk) {
+        const uint32_t off = (kk >> 2) * T * 128 / 16 + (kk & 3) * 2;
+        go(kk, kmajor_panel(tile) + off, off);
+    }
+    if constexpr (C::REST > 0)
+        if (ks > C::PANELS * 4) go(C::PANELS * 4, kmajor(tile + C::PANELS * T * 128, CH), 0u);
+}
+// One step of 16 tokens with v as B: N in one go, or the panel and the rest apart.  mma(d, b, idesc)
+template <int D, bool A_MN, class F>
+__device__ __forceinline__ void value_step(uint32_t d, uint32_t v, int kk, F mma)
+{
+    using C = Cfg<D>;
+    mma(d, mnmajor_panel(v) + kk * 128, idesc_bf16(128, C::PANELS * 64, A_MN, true));
+    if constexpr (C::REST > 0) mma(d + C::PANELS * 64, mnmajor(v + C::PANELS * T * 128, CH) + kk * 16, idesc_bf16(128, 16, A_MN, true));
+}
+// U (+)= KD^T V: M = 128, rows beyond the keys' channels are whatever follows in shared memory and are not used.
+template <int D>
+__device__ __forceinline__ void issue_state(uint32_t d, uint32_t kd, uint32_t v, bool accumulate)
+{
+    const uint64_t a = mnmajor(kd, CH);
+#pragma unroll 1
+    for (int kk = 0; kk < T / 16; ++kk)
+        value_step<D, true>(d, v, kk, [&](uint32_t dd, uint64_t b, uint32_t idesc) { mma_f16(dd, a + kk * 16, b, idesc, accumulate || kk > 0); });
+}
+
+// Decayed keys in PARTS parts of 8 bits: row j times g^(last - j).  Thread i of 256: one row, every second chunk.
+template <int D, int PARTS>
+__device__ __forceinline__ void decay_keys(int i, const char *K, char *out, int nch, float lam, int last)
+{
+    const int j = i & (T - 1);
+    const float w1 = exp2_of(lam * max(last - j, 0));
+    const float2 w = make_float2(w1, w1);
+#pragma unroll 1
+    for (int c = i / T; c < nch; c += 2) {
+        const uint4 u = *reinterpret_cast<const uint4 *>(K + chunk_at<D>(j, c));
+        uint32_t x[4] = {u.x, u.y, u.z, u.w}, y[PARTS][4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            float2 p = mul2(bf2(x[m]), w);
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part) {
+                y[part][m] = pack(p.x, p.y);
+                if (part + 1 < PARTS) p = sub2(p, bf2(y[part][m]));
+            }
+        }
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part)
+            *reinterpret_cast<uint4 *>(out + (part * nch + c) * CH + j * 16) = make_uint4(y[part][0], y[part][1], y[part][2], y[part][3]);
+    }
+}
+// 8 columns of a row of results in fp32.
+__device__ __forceinline__ void put8(float *p, const float *o)
+{
+    store4(p, make_float4(o[0], o[1], o[2], o[3]));
+    store4(p + 4, make_float4(o[4], o[5], o[6], o[7]));
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant__ Args a, int items, int *status)
+{
+    using C = Cfg<D>;
+    extern __shared__ char raw[];
+    __shared__ Ctl ctl;
+    char *sm = raw + (-smem_u32(raw) & 1023);
+    const uint32_t base = smem_u32(sm);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+    if (warp == 0) tmem_alloc(&ctl.tmem, 512);
     if (tid == 32) {
-        mbar_init(&ctl.bar[0], 1);
-        mbar_init(&ctl.bar[1], 1);
+        for (int j = 0; j < 2; ++j) {
+            mbar_init(&ctl.q[j], 32); mbar_init(&ctl.k[j], 32); mbar_init(&ctl.v[j], 32);
+            mbar_init(&ctl.s[j], 1); mbar_init(&ctl.i[j], 1); mbar_init(&ctl.u[j], 1); mbar_init(&ctl.o[j], 1);
+            mbar_init(&ctl.p[j], kScore); mbar_init(&ctl.kd[j], kState); mbar_init(&ctl.x[j], kState);
+            mbar_init(&ctl.uf[j], kState); mbar_init(&ctl.of[j], kOut);
+        }
         ctl.dead = 0;
         fence_barrier_init();
     }
-    for (int i = dk / 8 * T + tid; i < C::NCH * T; i += NT) {           // channels that are not there
-        zero16(Q + i / T * CH + i % T * 16);
-        zero16(K + i / T * CH + i % T * 16);
-    }
-    for (int i = dv / 8 * T + tid; i < C::NCH * T; i += NT) zero16(V + i / T * CH + i % T * 16);
-    float cw[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) cw[i] = exp2_of(lam * (15 - i));
-
     pdl_wait();
-    const int n = length_of(a.lengths, a.L, b), t0 = seg * a.G, t1 = min(t0 + a.G, (a.L + T - 1) / T), t_end = min(t1, (n + T - 1) / T);
-    const Src sq = src_of(ps.q, b, h, dk), sk = src_of(ps.k, b, h, dk), sv = src_of(ps.v, b, h, dv);
-    const size_t dd = (size_t)dk * dv;
-
-    // state: row `row`, columns half * HALF ...
-    float s[C::HALF];
-    const float *x0 = seg > 0 ? ps.local + ((size_t)bh * a.nseg + seg) * dd : ps.x0 ? ps.x0 + (size_t)bh * dd : nullptr;
-    const bool turned = seg > 0 ? ps.local_transposed : ps.x_transposed;
-#pragma unroll
-    for (int c = 0; c < C::HALF; ++c) {
-        const int col = half * C::HALF + c;
-        s[c] = x0 && row < dk && col < dv ? x0[turned ? (size_t)col * dk + row : (size_t)row * dv + col] : 0.f;
-    }
-    auto put_state = [&] {
-        if (row >= D) return;
-#pragma unroll
-        for (int c = 0; c < C::HALF; c += 8)
-            *reinterpret_cast<uint4 *>(X + (half * C::HALF + c) / 8 * C::CHX + row * 16) =
-                make_uint4(pack(s[c], s[c + 1]), pack(s[c + 2], s[c + 3]), pack(s[c + 4], s[c + 5]), pack(s[c + 6], s[c + 7]));
-    };
-    put_state();
-    tokens(ctl.tok[t0 & 1], a, ps.dir, t0, n);
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    const uint32_t tm = ctl.tmem, mine = tm + ((uint32_t)(quarter * 32) << 16);
-    if (t0 < t_end) {
-        load_tile(q, sq, ctl.tok[t0 & 1]);
-        load_tile(k, sk, ctl.tok[t0 & 1]);
-        copy_commit();
-        load_tile(v, sv, ctl.tok[t0 & 1]);
-        copy_commit();
-    }
-    for (int t = t0; t < t_end; ++t) {
-        const int p0 = t * T, rows = min(T, n - p0), lead = p0 == 0 ? ps.first : 1;
-        const uint32_t parity = (t - t0) & 1;
-        const bool has_state = t > t0 || x0, next = t + 1 < t_end, keep = next || ends;
-        copy_wait<1>();
-        fence_async_smem();
-        tc_fence_before_sync();
-        __syncthreads();
-        if (warp == 4 && elect_one()) {
-            tc_fence_after_sync();
-            const uint64_t qa = kmajor(q, CH), kb = kmajor(k, CH), xb = mnmajor(x, C::CHX);
-#pragma unroll
-            for (int kk = 0; kk < C::KS; ++kk) mma_f16(tm + C::S, qa + kk * (2 * CH / 16), kb + kk * (2 * CH / 16), idesc_bf16(128, T, false, false), kk > 0);
-            if (has_state) {
-#pragma unroll
-                for (int kk = 0; kk < C::KS; ++kk) mma_f16(tm + C::I, qa + kk * (2 * CH / 16), xb + kk * 16, idesc_bf16(128, D, false, true), kk > 0);
-            }
-            mma_commit(&ctl.bar[0]);
-        }
-        __syncwarp();
-        if (keep) decay_keys(K, KH, KL, dk / 8, lam, rows - 1, exact);
-        if (next) tokens(ctl.tok[(t + 1) & 1], a, ps.dir, t + 1, n);
-        wait(&ctl, 0, parity, status);
-        __syncthreads();                                     // q and k are free
-        tc_fence_after_sync();
-        if (next) {
-            load_tile(q, sq, ctl.tok[(t + 1) & 1]);
-            load_tile(k, sk, ctl.tok[(t + 1) & 1]);
-        }
-        copy_commit();
-        // decayed scores: keys 64 half .. of the row, in pairs of blocks of 16
-        for (int j0 = half * 64; j0 < min(half * 64 + 64, quarter * 32 + 32); j0 += 32) {
-            uint32_t r[2][16];
-            ld16(mine + C::S + j0, r[0]);
-            ld16(mine + C::S + j0 + 16, r[1]);
-            ld_wait();
-            const bool diagonal = j0 == quarter * 32;
-#pragma unroll
-            for (int g = 0; g < 2; ++g) {
-                uint32_t p[8];
-                if (diagonal) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int gap = row - (j0 + g * 16 + i);
-                        r[g][i] = __float_as_uint(gap >= 0 ? f(r[g][i]) * exp2_of(lam * gap) : 0.f);
+    const uint32_t tm = ctl.tmem;
+    int i = 0;                                   // tiles so far
+
+    if (warp >= kLoad && warp < kMma) {
+        const int which = warp - kLoad;          // q, k, v
+        for (int item = blockIdx.x; item < items; item += gridDim.x) {
+            const Item w = item_at(a, item);
+            const Pass &ps = a.pass[w.pass];
+            const Rows &r = which == 0 ? ps.q : which == 1 ? ps.k : ps.v;
+            const int d = which == 2 ? ps.dv : ps.dk;
+            for (int t = w.t0; t < w.t_end; ++t, ++i) {
+                const int old = i - C::STAGES;
+                if (old >= 0) {
+                    if (which < 2) wait(&ctl, ctl.i, old, status);
+                    if (which == 1) wait(&ctl, ctl.kd, old, status);
+                    if (which == 2) {
+                        wait(&ctl, ctl.u, old, status);
+                        wait(&ctl, ctl.o, old, status);
                     }
-                } else {
-                    const float w = exp2_of(lam * (row - (j0 + g * 16 + 15)));
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) r[g][i] = __float_as_uint(f(r[g][i]) * (w * cw[i]));
                 }
+                const uint32_t tile = (which * C::STAGES + i % C::STAGES) * C::TILE;
+                // q and k are summed over in steps of 16 channels: zeros where the last step has 8
+                if (which < 2 && (d & 8)) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) p[i] = pack(f(r[g][2 * i]), f(r[g][2 * i + 1]));
-                st8(mine + (half ? C::P1 : C::P0) + (j0 - half * 64) / 2 + g * 8, p);
+                    for (int j = 0; j < T / 32; ++j) zero16(sm + tile + chunk_at<D>(j * 32 + lane, d / 8));
+                }
+                load_tile<D>(a, base + tile, r, w, ps.dir, t, d);
+                copies_done();
+                arrive(which == 0 ? &ctl.q[i & 1] : which == 1 ? &ctl.k[i & 1] : &ctl.v[i & 1]);
             }
         }
-        // what the entering state gives
-        float o[C::HALF];
-        if (has_state) {
-            uint32_t r[C::HALF];
-#pragma unroll
-            for (int c = 0; c < C::HALF; c += 8) ld8(mine + C::I + half * C::HALF + c, r + c);
-            ld_wait();
-            const float w = exp2_of(lam * (row + lead));
-#pragma unroll
-            for (int c = 0; c < C::HALF; ++c) o[c] = f(r[c]) * w;
-        } else {
-#pragma unroll
-            for (int c = 0; c < C::HALF; ++c) o[c] = 0.f;
-        }
-        tmem_st_wait();
-        copy_wait<1>();                                      // v
-        fence_async_smem();                                  // v and the decayed keys
-        tc_fence_before_sync();
-        __syncthreads();
-        if (warp == 4 && elect_one()) {
+    } else if (warp == kMma) {
+        int ahead = 0;                           // tiles whose scores have been issued
+        auto scores = [&](int j, int ks) {       // of tile j
             tc_fence_after_sync();
-            const uint64_t vb = mnmajor(v, CH);
-            // keys 16 kk .. are behind the rows of the quarters below kk / 2: those stay as they are, so that no zero meets a NaN there
-#pragma unroll
-            for (int kk = 0; kk < T / 16; ++kk)
-                mma_ts(tm + C::O, tm + (kk < 4 ? C::P0 + kk * 8 : C::P1 + (kk - 4) * 8), vb + kk * 16, idesc_bf16(128, D, false, true), kk > 0, kk / 2);
-            if (keep) {
-                issue_state<D>(tm + C::I, kh, v, false);
-                if (exact) issue_state<D>(tm + C::I, kl, v, true);
+            const uint32_t q = base + C::Q + j % C::STAGES * C::TILE, k = base + C::K + j % C::STAGES * C::TILE, d = tm + C::S + j % C::S_BUFS * 128;
+            if (elect_one()) {
+                each_channel_step<D>(q, ks, [&](int kk, uint64_t qa, uint32_t off) {
+                    mma_f16(d, qa, C::REST > 0 && kk >= C::PANELS * 4 ? kmajor(k + C::PANELS * T * 128, CH) : kmajor_panel(k) + off, idesc_bf16(128, T, false, false), kk > 0);
+                });
+                mma_commit(&ctl.s[j & 1]);
             }
-            mma_commit(&ctl.bar[1]);
+            __syncwarp();
+            ++ahead;
+        };
+        for (int item = blockIdx.x; item < items; item += gridDim.x) {
+            const Item w = item_at(a, item);
+            const Pass &ps = a.pass[w.pass];
+            const bool start = w.seg > 0 || ps.x0;
+            const int ks = (ps.dk + 15) / 16;
+            for (int t = w.t0; t < w.t_end; ++t, ++i) {
+                const bool next = t + 1 < w.t_end;
+                const uint32_t q = base + C::Q + i % C::STAGES * C::TILE, v = base + C::V + i % C::STAGES * C::TILE;
+                if (ahead == i) {
+                    if (C::S_BUFS == 1 && i > 0) wait(&ctl, ctl.o, i - 1, status);          // the decayed scores before are used up
+                    wait(&ctl, ctl.q, i, status);
+                    wait(&ctl, ctl.k, i, status);
+                    scores(i, ks);
+                }
+                wait(&ctl, ctl.v, i, status);
+                if (next) {
+                    wait(&ctl, ctl.kd, i, status);
+                    if (i > 0) wait(&ctl, ctl.uf, i - 1, status);
+                }
+                tc_fence_after_sync();
+                if (elect_one()) {
+                    if (next) issue_state<D>(tm + C::U, base + C::KD + i % C::KEY_BUFS * C::KEYS, v, false);
+                    mma_commit(&ctl.u[i & 1]);
+                }
+                __syncwarp();
+                wait(&ctl, ctl.x, i, status);
+                if (i > 0) wait(&ctl, ctl.of, i - 1, status);
+                tc_fence_after_sync();
+                if (elect_one()) {
+                    if (t > w.t0 || start) {
+                        const uint64_t xh = mnmajor(base + C::X, C::CHX), xl = mnmajor(base + C::X + C::XT, C::CHX);
+                        each_channel_step<D>(q, ks, [&](int kk, uint64_t qa, uint32_t) {
+                            mma_f16(tm + C::I, qa, xh + kk * 16, idesc_bf16(128, D, false, true), kk > 0);
+                            mma_f16(tm + C::I, qa, xl + kk * 16, idesc_bf16(128, D, false, true), true);
+                        });
+                    }
+                    mma_commit(&ctl.i[i & 1]);
+                }
+                __syncwarp();
+                // The next tile's scores, where they need not be waited for.  The decayed scores that they take the place of were used up before
+                // the results that the wait above was for.
+                if (C::S_BUFS == 2 && next && ready(ctl.q, i + 1) && ready(ctl.k, i + 1)) scores(i + 1, ks);
+                wait(&ctl, ctl.p, i, status);
+                tc_fence_after_sync();
+                if (elect_one()) {
+                    // keys 16 kk .. are behind the rows of the quarters below kk / 2: those stay as they are, so that no zero meets a NaN there
+#pragma unroll 1
+                    for (int kk = 0; kk < T / 16; ++kk)
+                        value_step<D, false>(tm + C::O, v, kk, [&](uint32_t d, uint64_t b, uint32_t idesc) {
+                            mma_ts(d, tm + C::S + i % C::S_BUFS * 128 + p_col(kk), b, idesc, kk > 0, kk / 2);
+                        });
+                    mma_commit(&ctl.o[i & 1]);
+                }
+                __syncwarp();
+            }
         }
-        __syncwarp();
-        wait(&ctl, 1, parity, status);
-        tc_fence_after_sync();
-        if (next) load_tile(v, sv, ctl.tok[(t + 1) & 1]);
-        copy_commit();
-        {
-            uint32_t r[C::HALF];
+    } else if (warp < kScore) {
+        const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;
+        const uint32_t mine = tm + ((uint32_t)(quarter * 32) << 16);
+        for (int item = blockIdx.x; item < items; item += gridDim.x) {
+            const Item w = item_at(a, item);
+            const float lam = a.lam.v[w.h];
+            // Factors of a block's 16 keys, g^(row - j0 - 15) and g^15 .. g^0.  Within the diagonal block the first goes up to g^-31, beyond
+            // what fp32 holds where a position leaves less than 1/16: there the powers are formed one by one.
+            const bool strong = lam < -4.f;
+            float2 cw[8];
 #pragma unroll
-            for (int c = 0; c < C::HALF; c += 8) ld8(mine + C::O + half * C::HALF + c, r + c);
-            ld_wait();
-            const int p = p0 + row, tok = p < a.L ? token_at(a, ps.dir, p, n) : -1;
-            if (tok >= 0) {
-                const size_t at = (((size_t)b * a.L + tok) * a.H + h) * dv + half * C::HALF;
+            for (int j = 0; j < 8; ++j) cw[j] = make_float2(exp2_of(lam * (15 - 2 * j)), exp2_of(lam * (14 - 2 * j)));
+            for (int t = w.t0; t < w.t_end; ++t, ++i) {
+                const uint32_t sp = mine + C::S + i % C::S_BUFS * 128;
+                wait(&ctl, ctl.s, i, status);
+                tc_fence_after_sync();
+                // 16 keys at a time, of the blocks of 32 half and half + 2, where they are not behind the row
+#pragma unroll 1
+                for (int m = 0; m < 4; ++m) {
+                    const int block = half + (m & 2), g = m & 1, gap = row - (block * 32 + g * 16 + 15);
+                    if (block > quarter) break;
+                    uint32_t r[16], p[8];
+                    ld16(sp + block * 32 + g * 16, r);
+                    const float w1 = exp2_of(lam * gap);
+                    const float2 ww = make_float2(w1, w1);
+                    ld_wait();
+                    if (block == quarter && strong) {
 #pragma unroll
-                for (int c = 0; c < C::HALF; c += 8) {
-                    float y[8];
+                        for (int j = 0; j < 16; ++j) r[j] = __float_as_uint(f(r[j]) * exp2_of(lam * max(gap + 15 - j, 0)));
+                    } else {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) y[e] = p < n ? o[c + e] + f(r[c + e]) : 0.f;
-                    if (half * C::HALF + c < dv) put8(ps, at + c, y);
+                        for (int j = 0; j < 8; ++j) {
+                            const float2 y = mul2(make_float2(f(r[2 * j]), f(r[2 * j + 1])), mul2(ww, cw[j]));
+                            r[2 * j] = __float_as_uint(y.x);
+                            r[2 * j + 1] = __float_as_uint(y.y);
+                        }
+                    }
+                    if (block == quarter) {
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) r[j] = gap + 15 >= j ? r[j] : 0u;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) p[j] = pack(f(r[2 * j]), f(r[2 * j + 1]));
+                    st8(sp + p_col(2 * block + g), p);
+                }
+                tmem_st_wait();
+                tc_fence_before_sync();
+                warp_arrive(&ctl.p[i & 1]);
+            }
+        }
+    } else if (warp < kScore + kState) {
+        const int quarter = warp & 3, half = (warp >> 2) & 1, row = quarter * 32 + lane, me = tid - kScore * 32;
+        const uint32_t mine = tm + ((uint32_t)(quarter * 32) << 16);
+        char *X = sm + C::X;
+        float s[C::HALF];                        // state: row `row`, columns half * HALF ...; as an operand in two bf16 parts
+        auto put_state = [&](int dk) {
+            if (row >= dk) {                     // rows that are summed over all the same: up to a multiple of 16
+                if (row < (dk + 15) / 16 * 16) {
+#pragma unroll
+                    for (int c = 0; c < C::HALF; c += 8) {
+                        char *at = X + (half * C::HALF + c) / 8 * C::CHX + row * 16;
+                        zero16(at);
+                        zero16(at + C::XT);
+                    }
+                    fence_async_smem();
+                }
+                return;
+            }
+#pragma unroll
+            for (int c = 0; c < C::HALF; c += 8) {
+                uint32_t hi[4], lo[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float2 y = make_float2(s[c + 2 * j], s[c + 2 * j + 1]);
+                    hi[j] = pack(y.x, y.y);
+                    const float2 z = sub2(y, bf2(hi[j]));
+                    lo[j] = pack(z.x, z.y);
+                }
+                char *at = X + (half * C::HALF + c) / 8 * C::CHX + row * 16;
+                *reinterpret_cast<uint4 *>(at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                *reinterpret_cast<uint4 *>(at + C::XT) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            }
+            fence_async_smem();
+        };
+        for (int item = blockIdx.x; item < items; item += gridDim.x) {
+            const Item w = item_at(a, item);
+            if (w.t0 >= w.t_end) continue;
+            const Pass &ps = a.pass[w.pass];
+            const float lam = a.lam.v[w.h];
+            const int dk = ps.dk, dv = ps.dv, bh = w.b * a.H + w.h;
+            const float *x0 = w.seg > 0 ? ps.local + ((size_t)bh * a.nseg + w.seg) * dk * dv : ps.x0 ? ps.x0 + (size_t)bh * dk * dv : nullptr;
+            auto keys = [&](int t, int j) {      // of tile t, the list's tile j
+                wait(&ctl, ctl.k, j, status);
+                if (t + 1 < w.t_end) {
+                    decay_keys<D, 1>(me, sm + C::K + j % C::STAGES * C::TILE, sm + C::KD + j % C::KEY_BUFS * C::KEYS, dk / 8, lam, T - 1);
+                    fence_async_smem();
+                }
+                warp_arrive(&ctl.kd[j & 1]);
+            };
+            const bool turned = w.seg > 0 ? ps.local_transposed : ps.x_transposed;
+            if (x0 && turned) {
+#pragma unroll
+                for (int c = 0; c < C::HALF; ++c) {
+                    const int col = half * C::HALF + c;
+                    s[c] = row < dk && col < dv ? x0[col * dk + row] : 0.f;
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < C::HALF; c += 4) {
+                    const int col = half * C::HALF + c;
+                    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (x0 && row < dk && col < dv) y = *reinterpret_cast<const float4 *>(x0 + row * dv + col);
+                    s[c] = y.x; s[c + 1] = y.y; s[c + 2] = y.z; s[c + 3] = y.w;
+                }
+            }
+            if (i > 0) wait(&ctl, ctl.i, i - 1, status);             // the state before has been used
+            if (x0) put_state(dk);
+            warp_arrive(&ctl.x[i & 1]);
+            keys(w.t0, i);
+            for (int t = w.t0; t < w.t_end; ++t, ++i) {
+                const bool next = t + 1 < w.t_end;
+                if (C::KEY_BUFS == 2 && next) keys(t + 1, i + 1);
+                const float wn = exp2_of(lam * (T - 1 + (t == 0 ? ps.first : 1)));
+                wait(&ctl, ctl.u, i, status);
+                if (next && quarter * 32 < D) {
+                    tc_fence_after_sync();
+                    auto update = [&](int c, auto count) {
+                        constexpr int N = decltype(count)::value;
+                        uint32_t r[N];
+#pragma unroll
+                        for (int e = 0; e < N; e += 8) ld8(mine + C::U + half * C::HALF + c + e, r + e);
+                        ld_wait();
+#pragma unroll
+                        for (int e = 0; e < N; ++e) s[c + e] = fmaf(wn, s[c + e], f(r[e]));
+                    };
+#pragma unroll
+                    for (int c = 0; c + 16 <= C::HALF; c += 16) update(c, std::integral_constant<int, 16>());
+                    if constexpr (C::HALF % 16 != 0) update(C::HALF - 8, std::integral_constant<int, 8>());
+                    tc_fence_before_sync();
+                }
+                warp_arrive(&ctl.uf[i & 1]);
+                if (next) {
+                    wait(&ctl, ctl.i, i, status);
+                    put_state(dk);
+                    warp_arrive(&ctl.x[(i + 1) & 1]);
+                    if (C::KEY_BUFS == 1) keys(t + 1, i + 1);
                 }
             }
         }
-        if (keep && quarter * 32 < D) {
-            uint32_t r[C::HALF];
+    } else {
+        const int quarter = warp & 3, row = quarter * 32 + lane;
+        const uint32_t mine = tm + ((uint32_t)(quarter * 32) << 16);
+        char *R = sm + C::R;
+        for (int item = blockIdx.x; item < items; item += gridDim.x) {
+            const Item w = item_at(a, item);
+            const Pass &ps = a.pass[w.pass];
+            const float lam = a.lam.v[w.h];
+            const int dv = ps.dv, nch = dv / 8;
+            const bool start = w.seg > 0 || ps.x0;
+            const size_t tok_out = (size_t)a.H * dv, head_out = (size_t)w.b * a.L * tok_out + (size_t)w.h * dv;
+            for (int t = w.t0; t < w.t_end; ++t, ++i) {
+                const int p0 = t * T, rows = min(T, w.n - p0);
+                const bool has_state = t > w.t0 || start;
+                const float wr = exp2_of(lam * (row + (t == 0 ? ps.first : 1)));
+                const int mt = token_or_not(a, ps.dir, p0 + row, w.n), my_token = mt >= 0 ? mt : ~mt;
+                wait(&ctl, ctl.o, i, status);
+                tc_fence_after_sync();
+                sync_out_warps();                // the results before have been read
+                ctl.tok[row] = my_token;
+#pragma unroll 1
+                for (int c = 0; c < D; c += 16) {
+                    uint32_t r[16], y[16];
+                    ld16(mine + C::O + c, r);
+                    if (has_state) ld16(mine + C::I + c, y);
+                    ld_wait();
+                    if (c + 16 >= D) {
+                        tc_fence_before_sync();
+                        warp_arrive(&ctl.of[i & 1]);
+                    }
+                    if (has_state) {
+                        const float2 w2 = make_float2(wr, wr);
 #pragma unroll
-            for (int c = 0; c < C::HALF; c += 8) ld8(mine + C::I + half * C::HALF + c, r + c);
-            ld_wait();
-            const float w = exp2_of(lam * (rows - 1 + lead));
+                        for (int e = 0; e < 16; e += 2) {
+                            const float2 z = fma2(w2, make_float2(f(y[e]), f(y[e + 1])), make_float2(f(r[e]), f(r[e + 1])));
+                            r[e] = __float_as_uint(z.x);
+                            r[e + 1] = __float_as_uint(z.y);
+                        }
+                    }
+                    if (rows < T) {
 #pragma unroll
-            for (int c = 0; c < C::HALF; ++c) s[c] = row < dk ? fmaf(w, s[c], f(r[c])) : 0.f;
-            put_state();
+                        for (int e = 0; e < 16; ++e) r[e] = row < rows ? r[e] : 0u;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; e += 8) {
+                        const int ch = (c + e) / 8;
+                        if (ch >= nch) break;
+                        if (ps.out_f32) {
+                            if (my_token < a.L) put8((float *)ps.out + head_out + my_token * tok_out + ch * 8, reinterpret_cast<const float *>(r + e));
+                        } else {
+                            *reinterpret_cast<uint4 *>(R + ch * CH + row * 16) = make_uint4(pack(f(r[e]), f(r[e + 1])), pack(f(r[e + 2]), f(r[e + 3])), pack(f(r[e + 4]), f(r[e + 5])),
+                                                                                            pack(f(r[e + 6]), f(r[e + 7])));
+                        }
+                    }
+                }
+                sync_out_warps();
+                // Rows to global memory: consecutive lanes have the chunks of one.  (A bulk copy a row, issued by four warps, took 5700 cycles a tile.)
+                if (!ps.out_f32) {
+                    const int me = tid - (kScore + kState) * 32;
+                    constexpr int LANES = D == 128 ? 16 : 8, STEP = kOut * 32 / LANES;
+                    const int c = me % LANES;
+                    bf16 *out = (bf16 *)ps.out + head_out + c * 8;
+                    const char *from = R + c * CH;
+                    if (c < nch) {
+#pragma unroll 1
+                        for (int r0 = me / LANES; r0 < T; r0 += 8 * STEP) {
+                            int to[8];
+                            uint4 y[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                to[j] = ctl.tok[r0 + j * STEP];
+                                y[j] = *reinterpret_cast<const uint4 *>(from + (r0 + j * STEP) * 16);
+                            }
+#pragma unroll
+                            for (int j = 0; j < 8; ++j)
+                                if (to[j] < a.L) *reinterpret_cast<uint4 *>(out + to[j] * tok_out) = y[j];
+                        }
+                    }
+                    if constexpr (C::REST > 0) {             // chunks 8 and 9, a row a thread
+#pragma unroll
+                        for (int ch = LANES; ch < C::NCH; ++ch)
+                            if (ch < nch && my_token < a.L)
+                                *reinterpret_cast<uint4 *>((bf16 *)ps.out + head_out + my_token * tok_out + ch * 8) = *reinterpret_cast<const uint4 *>(R + ch * CH + row * 16);
+                    }
+                }
+            }
+            // whole tiles behind the end
+            for (int p = max(w.t_end, w.t0) * T + (warp - kScore - kState); p < min(w.t1 * T, a.L); p += kOut)
+                for (int c = lane * 8; c < dv; c += 256) {
+                    const float zero[8] = {};
+                    const size_t at = head_out + p * tok_out + c;
+                    if (ps.out_f32) put8((float *)ps.out + at, zero);
+                    else zero16((char *)((bf16 *)ps.out + at));
+                }
         }
     }
-    copy_wait<0>();
-    if (ends && row < dk) {
-        const float w = n > 0 && ps.last ? exp2_of(lam) : 1.f;            // no token: the start state
-#pragma unroll
-        for (int c = 0; c < C::HALF; ++c) {
-            const int col = half * C::HALF + c;
-            if (col < dv) ps.x_end[(size_t)bh * dd + (size_t)row * dv + col] = s[c] * w;
-        }
-    }
-    // whole tiles behind the end
-    for (int p = max(t_end, t0) * T + warp; p < min(t1 * T, a.L); p += NT / 32)
-        for (int c = lane * 8; c < dv; c += 256) {
-            const float y[8] = {};
-            put8(ps, (((size_t)b * a.L + p) * a.H + h) * dv + c, y);
-        }
     tc_fence_before_sync();
     __syncthreads();
     pdl_launch_dependents();
-    if (warp == 0) tmem_dealloc(tm, C::COLS);
+    if (warp == 0) tmem_dealloc(tm, 512);
 }
 
-// What a segment adds to the state behind it.
+// What a segment adds to the state behind it.  Where the final state is wanted (x_end), decayed keys in three parts.
+// Warps: 0 .. 7 decayed keys, 8 and 9 loads of k and v, 10 products.
 template <int D>
-__global__ void __launch_bounds__(NT, 2) decay_local(const __grid_constant__ Args a, int *status)
+struct LocalCfg {
+    // decayed keys first: their products read sixteen chunks from where a part starts, whatever stands there
+    static constexpr int COLS = D <= 64 ? 64 : 128, THREADS = 11 * 32;
+    __host__ __device__ static constexpr int keys(int parts, int nch) { return (parts * nch * CH + 1023) / 1024 * 1024; }
+    static constexpr int bytes(int parts, int nch) { return keys(parts, nch) + 4 * Cfg<D>::TILE + 1024; }
+    static_assert(keys(3, Cfg<D>::NCH) + 4 * Cfg<D>::TILE + 1024 + sizeof(Bars) <= 227 * 1024, "fits");
+};
+template <int D>
+__global__ void __launch_bounds__(LocalCfg<D>::THREADS, 2) decay_local(const __grid_constant__ Args a, int *status)
 {
     using C = Cfg<D>;
-    constexpr int COLS = D <= 64 ? 64 : 128;
-    extern __shared__ __align__(128) char sm[];
-    __shared__ Ctl ctl;
-    const Pass &ps = a.pass[blockIdx.x % a.passes];
-    const int seg = blockIdx.x / a.passes, bh = blockIdx.y, b = bh / a.H, h = bh - b * a.H, dk = ps.dk, dv = ps.dv;
-    const bool exact = true;
-    if (seg == a.nseg - 1 && !ps.x_end) {           // goes into the final state only
-        pdl_wait();
+    using LC = LocalCfg<D>;
+    extern __shared__ char raw[];
+    __shared__ Bars ctl;
+    char *sm = raw + (-smem_u32(raw) & 1023);
+    const uint32_t base = smem_u32(sm);
+    pdl_wait();
+    const Item w = item_at(a, blockIdx.x);
+    const Pass &ps = a.pass[w.pass];
+    const bool exact = ps.x_end;
+    if (w.seg == a.nseg - 1 && !exact) {         // goes into the final state only
         pdl_launch_dependents();
         return;
     }
-    const float lam = a.lam.v[h];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;
-    char *KH = sm, *KL = KH + dk / 8 * CH, *K = KL + (exact ? dk / 8 * CH : 0), *V = K + dk / 8 * CH;
-    const uint32_t kh = smem_u32(KH), kl = smem_u32(KL), k = smem_u32(K), v = smem_u32(V);
-    if (warp == 0) tmem_alloc(&ctl.tmem, COLS);
+    const int K0 = LC::keys(exact ? 3 : 1, ps.dk / 8), V0 = K0 + 2 * C::TILE;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, dk = ps.dk, dv = ps.dv, count = max(w.t_end - w.t0, 0), end = min((w.t0 + a.G) * T, w.n);
+    if (warp == 0) tmem_alloc(&ctl.tmem, LC::COLS);
     if (tid == 32) {
-        mbar_init(&ctl.bar[0], 1);
+        for (int j = 0; j < 2; ++j) {
+            mbar_init(&ctl.k[j], 32); mbar_init(&ctl.v[j], 32);
+            mbar_init(&ctl.o[j], 1); mbar_init(&ctl.kd[j], 8);
+        }
         ctl.dead = 0;
         fence_barrier_init();
     }
-    for (int i = dv / 8 * T + tid; i < C::NCH * T; i += NT) {
-        zero16(V + i / T * CH + i % T * 16);
-        zero16(V + C::TILE + i / T * CH + i % T * 16);
-    }
-    pdl_wait();
-    const int n = length_of(a.lengths, a.L, b), t0 = seg * a.G, t_end = min(t0 + a.G, (n + T - 1) / T), end = min((t0 + a.G) * T, n);
-    const Src sk = src_of(ps.k, b, h, dk), sv = src_of(ps.v, b, h, dv);
-    tokens(ctl.tok[t0 & 1], a, ps.dir, t0, n);
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    const uint32_t tm = ctl.tmem, mine = tm + ((uint32_t)(quarter * 32) << 16);
-    if (t0 < t_end) {
-        load_tile(k, sk, ctl.tok[t0 & 1]);
-        load_tile(v, sv, ctl.tok[t0 & 1]);
-    }
-    for (int t = t0; t < t_end; ++t) {
-        const int i = t - t0;
-        copy_wait_all();
-        if (t + 1 < t_end) tokens(ctl.tok[(t + 1) & 1], a, ps.dir, t + 1, n);
-        if (i > 0) wait(&ctl, 0, (i - 1) & 1, status);       // decayed keys and the other v are free
-        __syncthreads();
-        decay_keys(K, KH, KL, dk / 8, lam, end - 1 - t * T, exact);
-        fence_async_smem();
-        __syncthreads();
-        if (warp == 4 && elect_one()) {
+    const uint32_t tm = ctl.tmem;
+    if (warp == 8 || warp == 9) {
+        const bool value = warp == 9;
+        for (int i = 0; i < count; ++i) {
+            if (i >= 2) wait(&ctl, value ? ctl.o : ctl.kd, i - 2, status);
+            load_tile<D>(a, base + (value ? V0 : K0) + (i & 1) * C::TILE, value ? ps.v : ps.k, w, ps.dir, w.t0 + i, value ? dv : dk);
+            copies_done();
+            arrive(value ? &ctl.v[i & 1] : &ctl.k[i & 1]);
+        }
+    } else if (warp == 10) {
+        const uint32_t kd = base, part = dk / 8 * CH;
+        for (int i = 0; i < count; ++i) {
+            wait(&ctl, ctl.kd, i, status);
+            wait(&ctl, ctl.v, i, status);
+            if (elect_one()) {
+                tc_fence_after_sync();
+                const uint32_t v = base + V0 + (i & 1) * C::TILE;
+                issue_state<D>(tm, kd, v, i > 0);
+                if (exact) {
+                    issue_state<D>(tm, kd + part, v, true);
+                    issue_state<D>(tm, kd + 2 * part, v, true);
+                }
+                mma_commit(&ctl.o[i & 1]);
+            }
+            __syncwarp();
+        }
+    } else {
+        const float lam = a.lam.v[w.h];
+        const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;
+        const uint32_t mine = tm + ((uint32_t)(quarter * 32) << 16);
+        for (int i = 0; i < count; ++i) {
+            wait(&ctl, ctl.k, i, status);
+            if (i > 0) wait(&ctl, ctl.o, i - 1, status);         // decayed keys are free
+            const char *K = sm + K0 + (i & 1) * C::TILE;
+            if (exact) decay_keys<D, 3>(tid, K, sm, dk / 8, lam, end - 1 - (w.t0 + i) * T);
+            else decay_keys<D, 1>(tid, K, sm, dk / 8, lam, end - 1 - (w.t0 + i) * T);
+            fence_async_smem();
+            warp_arrive(&ctl.kd[i & 1]);
+        }
+        float *out = ps.local + ((size_t)(w.b * a.H + w.h) * a.nseg + w.seg) * dk * dv + (size_t)row * dv + half * C::HALF;
+        if (count > 0) {
+            wait(&ctl, ctl.o, count - 1, status);
             tc_fence_after_sync();
-            const uint32_t vt = v + (i & 1) * C::TILE;
-            issue_state<D>(tm, kh, vt, i > 0);
-            if (exact) issue_state<D>(tm, kl, vt, true);
-            mma_commit(&ctl.bar[0]);
         }
-        __syncwarp();
-        if (t + 1 < t_end) {
-            load_tile(k, sk, ctl.tok[(t + 1) & 1]);
-            load_tile(v + (~i & 1) * C::TILE, sv, ctl.tok[(t + 1) & 1]);
+#pragma unroll
+        for (int c = 0; c < C::HALF; c += 8) {
+            uint32_t r[8] = {};
+            if (count > 0) {
+                ld8(mine + half * C::HALF + c, r);
+                ld_wait();
+            }
+            if (row < dk && half * C::HALF + c < dv) put8(out + c, reinterpret_cast<const float *>(r));
         }
+        tc_fence_before_sync();
     }
-    if (t0 < t_end) {
-        wait(&ctl, 0, (t_end - 1 - t0) & 1, status);
-        tc_fence_after_sync();
-    }
-    float *out = ps.local + ((size_t)bh * a.nseg + seg) * dk * dv + (size_t)row * dv;
-    uint32_t r[C::HALF] = {};
-    if (t0 < t_end) {
-#pragma unroll
-        for (int c = 0; c < C::HALF; c += 8) ld8(mine + half * C::HALF + c, r + c);
-        ld_wait();
-    }
-    if (row < dk) {
-#pragma unroll
-        for (int c = 0; c < C::HALF; c += 4)
-            if (half * C::HALF + c < dv) store4(out + half * C::HALF + c, make_float4(f(r[c]), f(r[c + 1]), f(r[c + 2]), f(r[c + 3])));
-    }
-    tc_fence_before_sync();
     __syncthreads();
     pdl_launch_dependents();
-    if (warp == 0) tmem_dealloc(tm, COLS);
+    if (warp == 0) tmem_dealloc(tm, LC::COLS);
 }
 
 template <int D>
 dig_status launch(const Args &a, bool local, cudaStream_t stream)
 {
-    using C = Cfg<D>;
     int *status = device_status_ptr();
     if (!status) return DIG_ERR_CUDA;
-    size_t smem = 0;
-    for (int i = 0; i < a.passes; ++i) {
-        const Pass &p = a.pass[i];
-        const size_t keys = (size_t)p.dk / 8 * CH * 2;
-        // sixteen chunks from the start of the last part of the decayed keys are read
-        size_t need = local ? keys + (size_t)p.dk / 8 * CH + 2 * C::TILE : keys + 3 * C::TILE + C::XT;
-        const size_t read = keys - (size_t)p.dk / 8 * CH + 16 * CH;
-        need = need > read ? need : read;
-        smem = smem > need ? smem : need;
+    size_t smem = Cfg<D>::BYTES;
+    if (local) {
+        smem = 0;
+        for (int i = 0; i < a.passes; ++i) {
+            const size_t need = LocalCfg<D>::bytes(a.pass[i].x_end ? 3 : 1, a.pass[i].dk / 8);
+            smem = smem > need ? smem : need;
+        }
     }
     const void *fn = local ? (const void *)decay_local<D> : (const void *)decay_pass<D>;
     const dig_status st = ensure_dynamic_smem(fn, smem);
     if (st != DIG_OK) return st;
     KernelTimer t(local ? KID_DECAY_LOCAL : KID_DECAY, stream);
-    const dim3 grid(a.nseg * a.passes, a.B * a.H);
-    return cuda_ok(local ? launch_pdl(decay_local<D>, grid, dim3(NT), smem, stream, a, status) : launch_pdl(decay_pass<D>, grid, dim3(NT), smem, stream, a, status));
+    const long long items = (long long)a.nseg * a.passes * a.B * a.H;
+    if (local) return cuda_ok(launch_pdl(decay_local<D>, dim3((unsigned)items), dim3(LocalCfg<D>::THREADS), smem, stream, a, status));
+    return cuda_ok(launch_pdl(decay_pass<D>, dim3((unsigned)(items < kSms ? items : kSms)), dim3(kThreads), smem, stream, a, (int)items, status));
 }
 
 }  // namespace

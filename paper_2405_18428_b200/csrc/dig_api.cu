@@ -511,12 +511,12 @@ static bool decay_geometry_ok(int B, int H, int H_kv, int grid_h, int grid_w, in
 {
     return grid_h > 0 && grid_w > 0 && (long long)grid_h * grid_w <= (1ll << 24) && decay_sizes_ok(B, H, H_kv, d_k, d_v, dtype);
 }
-// Strides keep every row on a 16-byte boundary; inputs only, so rows may coincide.
+// Strides keep every row on a 16-byte boundary, and those of tokens fit 31 bits; inputs only, so rows may coincide.
 static bool strides_ok(const long long *s, int n, int dtype)
 {
     const int unit = dtype == DIG_F32 ? 4 : 8;
     for (int i = 0; s && i < n; ++i)
-        if (s[i] < 0 || s[i] % unit != 0) return false;
+        if (s[i] < 0 || s[i] % unit != 0 || (i % 2 && s[i] > 0x7fffffffll)) return false;
     return true;
 }
 
