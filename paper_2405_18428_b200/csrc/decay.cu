@@ -189,10 +189,14 @@ dig_status run(Args &a, const Carved &w, int n, int end, int dtype, cudaStream_t
     return pass_kernel(a, false, dtype, stream);
 }
 
+// The tensor-core kernels count results in 16 bytes with 32 bits.
+bool too_large(const DecayCall &c) { return c.dtype == DIG_BF16 && (size_t)c.B * c.L * c.H * (c.dk > c.dv ? c.dk : c.dv) / 8 >= 0xffffffffull; }
+
 }  // namespace
 
 dig_status decay_fwd_launch(const DecayCall &c)
 {
+    if (too_large(c)) return DIG_ERR_UNSUPPORTED;
     const int share = c.H / c.H_kv;
     const Carved w = carve(reinterpret_cast<char *>(c.ws), c.B, c.H, c.H_kv, c.L, c.dk, c.dv, c.dtype, false);
     Args a{};
@@ -210,6 +214,7 @@ dig_status decay_fwd_launch(const DecayCall &c)
 
 dig_status decay_bwd_launch(const DecayCall &c)
 {
+    if (too_large(c)) return DIG_ERR_UNSUPPORTED;
     const int share = c.H / c.H_kv;
     const Carved w = carve(reinterpret_cast<char *>(c.ws), c.B, c.H, c.H_kv, c.L, c.dk, c.dv, c.dtype, true);
     Args a{};

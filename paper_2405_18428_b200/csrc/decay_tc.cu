@@ -11,7 +11,7 @@
 //
 // One CTA per SM works through a list of segments; its warps have parts of their own, so that the loads of one tile, the scores of the
 // next, the state of this one and the results of the one before overlap:
-//   warps 0 .. 7    scores to decayed scores
+//   warps 0 .. 7    scores to decayed scores; results of the tile before to global memory
 //   warps 8 .. 15   decayed keys, state
 //   warps 16 .. 19  results
 //   warps 20 .. 22  loads of q, k, v;  warp 23  products
@@ -57,16 +57,19 @@ __device__ __forceinline__ constexpr int p_col(int kk) { return (kk >> 2) * 16 +
 
 // Barriers: two of each, tile i of the CTA's list uses i & 1 in phase i >> 1.  Nobody may be two phases behind on one: each is completed
 // again only after all that wait for it have gone on.
+constexpr uint32_t kNone = 0xffffffffu;
 struct Bars {
     uint64_t q[2], k[2], v[2];           // loaded
     uint64_t s[2], i[2], u[2], o[2];     // products done: scores; scores and what the state gives; the tile's state; outputs
     uint64_t p[2], kd[2], x[2];          // written: decayed scores, decayed keys, state
     uint64_t uf[2], of[2];               // read: the tile's state; outputs and what the state gives
+    uint64_t r[2], rf[2];                // results written to shared memory; read there
     uint32_t tmem;
     int dead;                            // a wait gave up: no more waiting
 };
 struct Ctl : Bars {
-    int tok[T];                          // token of every row of the tile whose results are on their way
+    uint32_t at[T];                      // rows of the tile whose results are on their way: in 16 bytes from the output's start, or kNone
+    int pass, nch;                       // its pass, and chunks of a row (0: they have gone out already)
 };
 
 __host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, bool a_mn, bool b_mn) { return idesc_f16(M, N, a_mn, b_mn) | (1u << 7) | (1u << 10); }
@@ -115,6 +118,8 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void *src, int bytes)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(dst), "l"(src), "r"(bytes) : "memory");
 }
+// One arrival once this thread's copies are there.  Who waits for it makes them visible to the tensor core.
+__device__ __forceinline__ void copies_arrive(uint64_t *bar) { asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" :: "r"(smem_u32(bar)) : "memory"); }
 // Until this thread's copies have arrived; then they are there for the tensor core too.
 __device__ __forceinline__ void copies_done()
 {
@@ -128,7 +133,6 @@ __device__ __forceinline__ void warp_arrive(uint64_t *bar)
     __syncwarp();
     if ((threadIdx.x & 31) == 0) arrive(bar);
 }
-__device__ __forceinline__ void sync_out_warps() { asm volatile("bar.sync 1, %0;" :: "n"(kOut * 32) : "memory"); }
 __device__ __forceinline__ void zero16(char *p) { *reinterpret_cast<uint4 *>(p) = make_uint4(0, 0, 0, 0); }
 
 __device__ __forceinline__ bool passed(uint64_t *bar, uint32_t parity)
@@ -303,10 +307,19 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
             mbar_init(&ctl.q[j], 32); mbar_init(&ctl.k[j], 32); mbar_init(&ctl.v[j], 32);
             mbar_init(&ctl.s[j], 1); mbar_init(&ctl.i[j], 1); mbar_init(&ctl.u[j], 1); mbar_init(&ctl.o[j], 1);
             mbar_init(&ctl.p[j], kScore); mbar_init(&ctl.kd[j], kState); mbar_init(&ctl.x[j], kState);
-            mbar_init(&ctl.uf[j], kState); mbar_init(&ctl.of[j], kOut);
+            mbar_init(&ctl.uf[j], kState); mbar_init(&ctl.of[j], kOut); mbar_init(&ctl.r[j], kOut); mbar_init(&ctl.rf[j], kScore);
         }
         ctl.dead = 0;
         fence_barrier_init();
+    }
+    // q and k are summed over in steps of 16 channels: zeros where the last step has 8.  Where the passes have keys of different sizes,
+    // with every tile.
+    bool alike = true;
+    for (int j = 1; j < a.passes; ++j) alike &= a.pass[j].dk == a.pass[0].dk;
+    const int odd = a.pass[0].dk & 8 ? a.pass[0].dk / 8 : 0;
+    if (alike && odd) {
+        for (int j = tid; j < 2 * C::STAGES * T; j += kThreads) zero16(sm + j / T * C::TILE + chunk_at<D>(j % T, odd));
+        fence_async_smem();
     }
     pdl_wait();
     tc_fence_before_sync();
@@ -333,20 +346,25 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
                     }
                 }
                 const uint32_t tile = (which * C::STAGES + i % C::STAGES) * C::TILE;
-                // q and k are summed over in steps of 16 channels: zeros where the last step has 8
-                if (which < 2 && (d & 8)) {
-#pragma unroll
-                    for (int j = 0; j < T / 32; ++j) zero16(sm + tile + chunk_at<D>(j * 32 + lane, d / 8));
-                }
+                uint64_t *bar = which == 0 ? &ctl.q[i & 1] : which == 1 ? &ctl.k[i & 1] : &ctl.v[i & 1];
                 load_tile<D>(a, base + tile, r, w, ps.dir, t, d);
-                copies_done();
-                arrive(which == 0 ? &ctl.q[i & 1] : which == 1 ? &ctl.k[i & 1] : &ctl.v[i & 1]);
+                if (alike) {
+                    copies_arrive(bar);
+                } else {
+                    if (which < 2 && (d & 8)) {
+#pragma unroll
+                        for (int j = 0; j < T / 32; ++j) zero16(sm + tile + chunk_at<D>(j * 32 + lane, d / 8));
+                    }
+                    copies_done();
+                    arrive(bar);
+                }
             }
         }
     } else if (warp == kMma) {
         int ahead = 0;                           // tiles whose scores have been issued
         auto scores = [&](int j, int ks) {       // of tile j
             tc_fence_after_sync();
+            fence_async_smem();                  // q and k, as they have been waited for
             const uint32_t q = base + C::Q + j % C::STAGES * C::TILE, k = base + C::K + j % C::STAGES * C::TILE, d = tm + C::S + j % C::S_BUFS * 128;
             if (elect_one()) {
                 each_channel_step<D>(q, ks, [&](int kk, uint64_t qa, uint32_t off) {
@@ -372,6 +390,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
                     scores(i, ks);
                 }
                 wait(&ctl, ctl.v, i, status);
+                fence_async_smem();
                 if (next) {
                     wait(&ctl, ctl.kd, i, status);
                     if (i > 0) wait(&ctl, ctl.uf, i - 1, status);
@@ -416,6 +435,35 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
     } else if (warp < kScore) {
         const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;
         const uint32_t mine = tm + ((uint32_t)(quarter * 32) << 16);
+        // Results of tile j from shared to global memory: consecutive lanes have the chunks of a row.  (A bulk copy a row, issued by four warps,
+        // took 5700 cycles a tile.)
+        auto rows_out = [&](int j) {
+            wait(&ctl, ctl.r, j, status);
+            constexpr int LANES = D == 128 ? 16 : 8, STEP = kScore * 32 / LANES;
+            const int nch = ctl.nch, c = tid % LANES;
+            char *out = (char *)a.pass[ctl.pass].out;
+            const char *from = sm + C::R + c * CH;
+            if (c < nch) {
+#pragma unroll 1
+                for (int r0 = tid / LANES; r0 < T; r0 += 4 * STEP) {
+                    uint32_t at[4];
+                    uint4 y[4];
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+                        at[m] = ctl.at[r0 + m * STEP];
+                        y[m] = *reinterpret_cast<const uint4 *>(from + (r0 + m * STEP) * 16);
+                    }
+#pragma unroll
+                    for (int m = 0; m < 4; ++m)
+                        if (at[m] != kNone) *reinterpret_cast<uint4 *>(out + (size_t)(at[m] + c) * 16) = y[m];
+                }
+            }
+            if constexpr (C::REST > 0) {         // chunks 8 and 9, a row a thread
+                const int ch = LANES + tid / T, r0 = tid % T;
+                if (ch < nch && ctl.at[r0] != kNone) *reinterpret_cast<uint4 *>(out + (size_t)(ctl.at[r0] + ch) * 16) = *reinterpret_cast<const uint4 *>(sm + C::R + ch * CH + r0 * 16);
+            }
+            warp_arrive(&ctl.rf[j & 1]);
+        };
         for (int item = blockIdx.x; item < items; item += gridDim.x) {
             const Item w = item_at(a, item);
             const float lam = a.lam.v[w.h];
@@ -461,8 +509,10 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
                 tmem_st_wait();
                 tc_fence_before_sync();
                 warp_arrive(&ctl.p[i & 1]);
+                if (i > 0) rows_out(i - 1);
             }
         }
+        if (i > 0) rows_out(i - 1);
     } else if (warp < kScore + kState) {
         const int quarter = warp & 3, half = (warp >> 2) & 1, row = quarter * 32 + lane, me = tid - kScore * 32;
         const uint32_t mine = tm + ((uint32_t)(quarter * 32) << 16);
@@ -577,11 +627,17 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
                 const int p0 = t * T, rows = min(T, w.n - p0);
                 const bool has_state = t > w.t0 || start;
                 const float wr = exp2_of(lam * (row + (t == 0 ? ps.first : 1)));
-                const int mt = token_or_not(a, ps.dir, p0 + row, w.n), my_token = mt >= 0 ? mt : ~mt;
+                const float2 w2 = make_float2(wr, wr);
+                const int mt = token_or_not(a, ps.dir, p0 + row, w.n), token = mt >= 0 ? mt : ~mt;
+                const size_t at = head_out + (size_t)token * tok_out;
+                if (i > 0) wait(&ctl, ctl.rf, i - 1, status);        // the results before have been read
                 wait(&ctl, ctl.o, i, status);
                 tc_fence_after_sync();
-                sync_out_warps();                // the results before have been read
-                ctl.tok[row] = my_token;
+                ctl.at[row] = token < a.L ? (uint32_t)(at / 8) : kNone;
+                if (tid == (kScore + kState) * 32) {
+                    ctl.pass = w.pass;
+                    ctl.nch = ps.out_f32 ? 0 : nch;
+                }
 #pragma unroll 1
                 for (int c = 0; c < D; c += 16) {
                     uint32_t r[16], y[16];
@@ -593,7 +649,6 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
                         warp_arrive(&ctl.of[i & 1]);
                     }
                     if (has_state) {
-                        const float2 w2 = make_float2(wr, wr);
 #pragma unroll
                         for (int e = 0; e < 16; e += 2) {
                             const float2 z = fma2(w2, make_float2(f(y[e]), f(y[e + 1])), make_float2(f(r[e]), f(r[e + 1])));
@@ -605,48 +660,18 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
 #pragma unroll
                         for (int e = 0; e < 16; ++e) r[e] = row < rows ? r[e] : 0u;
                     }
+                    if (ps.out_f32) {
 #pragma unroll
-                    for (int e = 0; e < 16; e += 8) {
-                        const int ch = (c + e) / 8;
-                        if (ch >= nch) break;
-                        if (ps.out_f32) {
-                            if (my_token < a.L) put8((float *)ps.out + head_out + my_token * tok_out + ch * 8, reinterpret_cast<const float *>(r + e));
-                        } else {
-                            *reinterpret_cast<uint4 *>(R + ch * CH + row * 16) = make_uint4(pack(f(r[e]), f(r[e + 1])), pack(f(r[e + 2]), f(r[e + 3])), pack(f(r[e + 4]), f(r[e + 5])),
-                                                                                            pack(f(r[e + 6]), f(r[e + 7])));
-                        }
+                        for (int e = 0; e < 16; e += 8)
+                            if (token < a.L && c + e < dv) put8((float *)ps.out + at + c + e, reinterpret_cast<const float *>(r + e));
+                        continue;
                     }
+#pragma unroll
+                    for (int e = 0; e < 16; e += 8)
+                        *reinterpret_cast<uint4 *>(R + (c + e) / 8 * CH + row * 16) = make_uint4(pack(f(r[e]), f(r[e + 1])), pack(f(r[e + 2]), f(r[e + 3])), pack(f(r[e + 4]), f(r[e + 5])),
+                                                                                                pack(f(r[e + 6]), f(r[e + 7])));
                 }
-                sync_out_warps();
-                // Rows to global memory: consecutive lanes have the chunks of one.  (A bulk copy a row, issued by four warps, took 5700 cycles a tile.)
-                if (!ps.out_f32) {
-                    const int me = tid - (kScore + kState) * 32;
-                    constexpr int LANES = D == 128 ? 16 : 8, STEP = kOut * 32 / LANES;
-                    const int c = me % LANES;
-                    bf16 *out = (bf16 *)ps.out + head_out + c * 8;
-                    const char *from = R + c * CH;
-                    if (c < nch) {
-#pragma unroll 1
-                        for (int r0 = me / LANES; r0 < T; r0 += 8 * STEP) {
-                            int to[8];
-                            uint4 y[8];
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                to[j] = ctl.tok[r0 + j * STEP];
-                                y[j] = *reinterpret_cast<const uint4 *>(from + (r0 + j * STEP) * 16);
-                            }
-#pragma unroll
-                            for (int j = 0; j < 8; ++j)
-                                if (to[j] < a.L) *reinterpret_cast<uint4 *>(out + to[j] * tok_out) = y[j];
-                        }
-                    }
-                    if constexpr (C::REST > 0) {             // chunks 8 and 9, a row a thread
-#pragma unroll
-                        for (int ch = LANES; ch < C::NCH; ++ch)
-                            if (ch < nch && my_token < a.L)
-                                *reinterpret_cast<uint4 *>((bf16 *)ps.out + head_out + my_token * tok_out + ch * 8) = *reinterpret_cast<const uint4 *>(R + ch * CH + row * 16);
-                    }
-                }
+                warp_arrive(&ctl.r[i & 1]);
             }
             // whole tiles behind the end
             for (int p = max(w.t_end, w.t0) * T + (warp - kScore - kState); p < min(w.t1 * T, a.L); p += kOut)
@@ -711,14 +736,14 @@ __global__ void __launch_bounds__(LocalCfg<D>::THREADS, 2) decay_local(const __g
         for (int i = 0; i < count; ++i) {
             if (i >= 2) wait(&ctl, value ? ctl.o : ctl.kd, i - 2, status);
             load_tile<D>(a, base + (value ? V0 : K0) + (i & 1) * C::TILE, value ? ps.v : ps.k, w, ps.dir, w.t0 + i, value ? dv : dk);
-            copies_done();
-            arrive(value ? &ctl.v[i & 1] : &ctl.k[i & 1]);
+            copies_arrive(value ? &ctl.v[i & 1] : &ctl.k[i & 1]);
         }
     } else if (warp == 10) {
         const uint32_t kd = base, part = dk / 8 * CH;
         for (int i = 0; i < count; ++i) {
             wait(&ctl, ctl.kd, i, status);
             wait(&ctl, ctl.v, i, status);
+            fence_async_smem();
             if (elect_one()) {
                 tc_fence_after_sync();
                 const uint32_t v = base + V0 + (i & 1) * C::TILE;
