@@ -174,16 +174,23 @@ Rows rows_of(const void *p, const long long *strides, long long L, int heads, in
 dig_status run(Args &a, const Carved &w, int n, int end, int dtype, cudaStream_t stream)
 {
     a.nseg = w.plan.nseg; a.G = w.plan.G;
-    Args l = a;
-    l.passes = a.nseg > 1 ? n : 0;
-    for (int i = 0; i < l.passes; ++i) l.pass[i].x_end = nullptr;
-    if (a.pass[end].x_end) {
-        l.pass[l.passes] = a.pass[end];
-        l.pass[l.passes++].local = w.final;
-    }
-    if (l.passes > 0) {
+    Pass &last = a.pass[end];
+    const bool cut = a.nseg > 1;
+    if (last.x_end) last.final = w.final;
+    if (cut || last.x_end) {
+        Args l = a;
+        l.passes = cut ? n : 1;
+        if (!cut) l.pass[0] = last;
         dig_status st = pass_kernel(l, true, dtype, stream);
-        if (st == DIG_OK) st = launch_scan(l, w.plan.tile, stream);
+        if (st != DIG_OK) return st;
+        // the scan: entering states of n passes, and the final one
+        l.passes = cut ? n : 0;
+        for (int i = 0; i < l.passes; ++i) l.pass[i].x_end = nullptr;
+        if (last.x_end) {
+            l.pass[l.passes] = last;
+            l.pass[l.passes++].local = w.final;
+        }
+        st = launch_scan(l, w.plan.tile, stream);
         if (st != DIG_OK) return st;
     }
     return pass_kernel(a, false, dtype, stream);

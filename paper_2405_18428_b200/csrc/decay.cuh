@@ -33,14 +33,15 @@ struct Rows {
 
 // One linear attention.  `dir`: its scan order; x0: start state [B][H][dk][dv] (transposed: [dv][dk]) or null, in force with
 // g^(p + first) at position p.  out: [B][L][H][dv], of the storage type, or fp32 where out_f32.  local: [B*H][nseg][dk][dv] fp32, written
-// by the local pass and turned into the entering states by the scan; `from`: the pass whose entering states this one reads
+// by the local pass (where there are several segments) and turned into the entering states by the scan; `from`: the pass whose entering states this one reads
 // (transposed where they differ).
 struct Pass {
     Rows q, k, v;
     void *out;
     const float *x0;
     float *local;
-    float *x_end;                        // where wanted: g^last (state behind the last position); in the scan alone
+    float *x_end;                        // scan: where wanted, g^last (state behind the last position), instead of the entering states
+    float *final;                        // local pass: where the final state is wanted, what adds up to it, [B*H][nseg][dk][dv] in fp32 accuracy
     int dk, dv, dir, first, last, x_transposed, local_transposed, out_f32;
 };
 

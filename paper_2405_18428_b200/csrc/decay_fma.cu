@@ -30,7 +30,7 @@ __device__ __forceinline__ float4 scaled(float4 x, float w) { return make_float4
 template <bool LOCAL>
 __global__ void __launch_bounds__(NT) decay_fma(const __grid_constant__ Args a)
 {
-    if (LOCAL && blockIdx.x == a.nseg - 1 && !a.pass[blockIdx.z].x_end) {            // goes into the final state only
+    if (LOCAL && blockIdx.x == a.nseg - 1 && !a.pass[blockIdx.z].final) {            // goes into the final state only
         pdl_wait();
         pdl_launch_dependents();
         return;
@@ -133,7 +133,12 @@ __global__ void __launch_bounds__(NT) decay_fma(const __grid_constant__ Args a)
     }
     __syncthreads();
     if (LOCAL) {
-        for (int i = tid; i < dk * dv; i += NT) local[i] = X[i / dv * ldv + i % dv];
+        float *whole = ps.final ? ps.final + ((size_t)bh * a.nseg + seg) * dd : nullptr;
+        for (int i = tid; i < dk * dv; i += NT) {
+            const float x = X[i / dv * ldv + i % dv];
+            if (a.nseg > 1) local[i] = x;
+            if (whole) whole[i] = x;
+        }
     }
     pdl_launch_dependents();
 }

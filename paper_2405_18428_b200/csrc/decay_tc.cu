@@ -233,10 +233,10 @@ template <int D, class F>
 __device__ __forceinline__ void each_channel_step(uint32_t tile, int ks, F go)
 {
     using C = Cfg<D>;
-#pragma unroll 1
-    for (int kk = 0; kk < (C::REST > 0 ? min(ks, C::PANELS * 4) : ks); ++kk) {
+#pragma unroll (D == 128 ? 1 : 8)
+    for (int kk = 0; kk < C::PANELS * 4; ++kk) {
         const uint32_t off = (kk >> 2) * T * 128 / 16 + (kk & 3) * 2;
-        go(kk, kmajor_panel(tile) + off, off);
+        if (kk < ks) go(kk, kmajor_panel(tile) + off, off);
     }
     if constexpr (C::REST > 0)
         if (ks > C::PANELS * 4) go(C::PANELS * 4, kmajor(tile + C::PANELS * T * 128, CH), 0u);
@@ -254,7 +254,7 @@ template <int D>
 __device__ __forceinline__ void issue_state(uint32_t d, uint32_t kd, uint32_t v, bool accumulate)
 {
     const uint64_t a = mnmajor(kd, CH);
-#pragma unroll 1
+#pragma unroll (D == 128 ? 1 : 8)
     for (int kk = 0; kk < T / 16; ++kk)
         value_step<D, true>(d, v, kk, [&](uint32_t dd, uint64_t b, uint32_t idesc) { mma_f16(dd, a + kk * 16, b, idesc, accumulate || kk > 0); });
 }
@@ -361,6 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
             }
         }
     } else if (warp == kMma) {
+        const uint32_t tm = warp_uniform(ctl.tmem), base = warp_uniform(smem_u32(sm));       // operands in uniform registers
         int ahead = 0;                           // tiles whose scores have been issued
         auto scores = [&](int j, int ks) {       // of tile j
             tc_fence_after_sync();
@@ -422,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
                 tc_fence_after_sync();
                 if (elect_one()) {
                     // keys 16 kk .. are behind the rows of the quarters below kk / 2: those stay as they are, so that no zero meets a NaN there
-#pragma unroll 1
+#pragma unroll (D == 128 ? 1 : 8)
                     for (int kk = 0; kk < T / 16; ++kk)
                         value_step<D, false>(tm + C::O, v, kk, [&](uint32_t d, uint64_t b, uint32_t idesc) {
                             mma_ts(d, tm + C::S + i % C::S_BUFS * 128 + p_col(kk), b, idesc, kk > 0, kk / 2);
@@ -689,18 +690,21 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
     if (warp == 0) tmem_dealloc(tm, 512);
 }
 
-// What a segment adds to the state behind it.  Where the final state is wanted (x_end), decayed keys in three parts.
-// Warps: 0 .. 7 decayed keys, 8 and 9 loads of k and v, 10 products.
+// What a segment adds to the state behind it: for the states that enter segments with the decayed keys in bf16, and where the final state
+// is wanted besides with two more parts of them, 24 bits, in accumulators of their own.
+// Warps: 0 .. 7 decayed keys, sums to global memory; 8 and 9 loads of k and v; 10 products.
 template <int D>
 struct LocalCfg {
     // decayed keys first: their products read sixteen chunks from where a part starts, whatever stands there
-    static constexpr int COLS = D <= 64 ? 64 : 128, THREADS = 11 * 32;
+    static constexpr int THREADS = 11 * 32;
     __host__ __device__ static constexpr int keys(int parts, int nch) { return (parts * nch * CH + 1023) / 1024 * 1024; }
     static constexpr int bytes(int parts, int nch) { return keys(parts, nch) + 4 * Cfg<D>::TILE + 1024; }
+    // tensor memory: two items' accumulators, of one part or of both
+    __host__ __device__ static constexpr int cols(bool exact) { return exact ? (D <= 64 ? 256 : 512) : D <= 64 ? 128 : 256; }
     static_assert(keys(3, Cfg<D>::NCH) + 4 * Cfg<D>::TILE + 1024 + sizeof(Bars) <= 227 * 1024, "fits");
 };
 template <int D>
-__global__ void __launch_bounds__(LocalCfg<D>::THREADS, 2) decay_local(const __grid_constant__ Args a, int *status)
+__global__ void __launch_bounds__(LocalCfg<D>::THREADS, 2) decay_local(const __grid_constant__ Args a, int items, int *status)
 {
     using C = Cfg<D>;
     using LC = LocalCfg<D>;
@@ -708,86 +712,135 @@ __global__ void __launch_bounds__(LocalCfg<D>::THREADS, 2) decay_local(const __g
     __shared__ Bars ctl;
     char *sm = raw + (-smem_u32(raw) & 1023);
     const uint32_t base = smem_u32(sm);
-    pdl_wait();
-    const Item w = item_at(a, blockIdx.x);
-    const Pass &ps = a.pass[w.pass];
-    const bool exact = ps.x_end;
-    if (w.seg == a.nseg - 1 && !exact) {         // goes into the final state only
-        pdl_launch_dependents();
-        return;
+    bool any_final = false;
+    int most = 0;
+    for (int j = 0; j < a.passes; ++j) {
+        any_final |= a.pass[j].final != nullptr;
+        most = max(most, a.pass[j].dk);
     }
-    const int K0 = LC::keys(exact ? 3 : 1, ps.dk / 8), V0 = K0 + 2 * C::TILE;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, dk = ps.dk, dv = ps.dv, count = max(w.t_end - w.t0, 0), end = min((w.t0 + a.G) * T, w.n);
-    if (warp == 0) tmem_alloc(&ctl.tmem, LC::COLS);
+    const int K0 = LC::keys(any_final ? 3 : 1, most / 8), V0 = K0 + 2 * C::TILE, cols = LC::cols(any_final);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (warp == 0) tmem_alloc(&ctl.tmem, cols);
     if (tid == 32) {
         for (int j = 0; j < 2; ++j) {
             mbar_init(&ctl.k[j], 32); mbar_init(&ctl.v[j], 32);
-            mbar_init(&ctl.o[j], 1); mbar_init(&ctl.kd[j], 8);
+            mbar_init(&ctl.o[j], 1); mbar_init(&ctl.kd[j], 8); mbar_init(&ctl.of[j], 8);
         }
         ctl.dead = 0;
         fence_barrier_init();
     }
+    pdl_wait();
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tm = ctl.tmem;
+    // Tiles whose tokens all count with a power of the decay that is 0 in fp32 are left out.
+    auto next_item = [&](int item, Item &w, int &end) {
+        w = item_at(a, item);
+        end = min((w.t0 + a.G) * T, w.n);
+        if (w.seg == a.nseg - 1 && !a.pass[w.pass].final) w.t_end = w.t0 = w.t1;           // goes into the final state only
+        const float lam = a.lam.v[w.h];
+        if (lam * (float)(end - w.t0 * T) < -130.f) {
+            const int far = end - ((int)(-130.f / lam) + 2) - T;             // tiles up to that of this position
+            if (far >= 0) w.t0 = max(w.t0, far / T + 1);
+        }
+    };
+    int i = 0, done = 0;                         // tiles and items with any so far
     if (warp == 8 || warp == 9) {
         const bool value = warp == 9;
-        for (int i = 0; i < count; ++i) {
-            if (i >= 2) wait(&ctl, value ? ctl.o : ctl.kd, i - 2, status);
-            load_tile<D>(a, base + (value ? V0 : K0) + (i & 1) * C::TILE, value ? ps.v : ps.k, w, ps.dir, w.t0 + i, value ? dv : dk);
-            copies_arrive(value ? &ctl.v[i & 1] : &ctl.k[i & 1]);
+        for (int item = blockIdx.x; item < items; item += gridDim.x) {
+            Item w;
+            int end;
+            next_item(item, w, end);
+            const Pass &ps = a.pass[w.pass];
+            for (int t = w.t0; t < w.t_end; ++t, ++i) {
+                if (i >= 2) wait(&ctl, value ? ctl.o : ctl.kd, i - 2, status);
+                load_tile<D>(a, base + (value ? V0 : K0) + (i & 1) * C::TILE, value ? ps.v : ps.k, w, ps.dir, t, value ? ps.dv : ps.dk);
+                copies_arrive(value ? &ctl.v[i & 1] : &ctl.k[i & 1]);
+            }
         }
     } else if (warp == 10) {
-        const uint32_t kd = base, part = dk / 8 * CH;
-        for (int i = 0; i < count; ++i) {
-            wait(&ctl, ctl.kd, i, status);
-            wait(&ctl, ctl.v, i, status);
-            fence_async_smem();
-            if (elect_one()) {
+        const uint32_t tm = warp_uniform(ctl.tmem), kd = warp_uniform(smem_u32(sm));
+        for (int item = blockIdx.x; item < items; item += gridDim.x) {
+            Item w;
+            int end;
+            next_item(item, w, end);
+            if (w.t0 >= w.t_end) continue;
+            const Pass &ps = a.pass[w.pass];
+            const uint32_t acc = tm + (done & 1) * (cols / 2), part = ps.dk / 8 * CH;
+            if (done >= 2) wait(&ctl, ctl.of, done - 2, status);
+            ++done;
+            for (int t = w.t0; t < w.t_end; ++t, ++i) {
+                wait(&ctl, ctl.kd, i, status);
+                wait(&ctl, ctl.v, i, status);
+                fence_async_smem();
                 tc_fence_after_sync();
-                const uint32_t v = base + V0 + (i & 1) * C::TILE;
-                issue_state<D>(tm, kd, v, i > 0);
-                if (exact) {
-                    issue_state<D>(tm, kd + part, v, true);
-                    issue_state<D>(tm, kd + 2 * part, v, true);
+                if (elect_one()) {
+                    const uint32_t v = kd + V0 + (i & 1) * C::TILE;
+                    issue_state<D>(acc, kd, v, t > w.t0);
+                    if (ps.final)
+#pragma unroll 1
+                        for (int j = 1; j < 3; ++j) issue_state<D>(acc + D, kd + j * part, v, t > w.t0 || j > 1);
+                    mma_commit(&ctl.o[i & 1]);
                 }
-                mma_commit(&ctl.o[i & 1]);
+                __syncwarp();
             }
-            __syncwarp();
         }
     } else {
-        const float lam = a.lam.v[w.h];
         const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;
-        const uint32_t mine = tm + ((uint32_t)(quarter * 32) << 16);
-        for (int i = 0; i < count; ++i) {
-            wait(&ctl, ctl.k, i, status);
-            if (i > 0) wait(&ctl, ctl.o, i - 1, status);         // decayed keys are free
-            const char *K = sm + K0 + (i & 1) * C::TILE;
-            if (exact) decay_keys<D, 3>(tid, K, sm, dk / 8, lam, end - 1 - (w.t0 + i) * T);
-            else decay_keys<D, 1>(tid, K, sm, dk / 8, lam, end - 1 - (w.t0 + i) * T);
-            fence_async_smem();
-            warp_arrive(&ctl.kd[i & 1]);
-        }
-        float *out = ps.local + ((size_t)(w.b * a.H + w.h) * a.nseg + w.seg) * dk * dv + (size_t)row * dv + half * C::HALF;
-        if (count > 0) {
-            wait(&ctl, ctl.o, count - 1, status);
-            tc_fence_after_sync();
-        }
-#pragma unroll
-        for (int c = 0; c < C::HALF; c += 8) {
-            uint32_t r[8] = {};
-            if (count > 0) {
-                ld8(mine + half * C::HALF + c, r);
-                ld_wait();
+        for (int item = blockIdx.x; item < items; item += gridDim.x) {
+            Item w;
+            int end;
+            next_item(item, w, end);
+            const Pass &ps = a.pass[w.pass];
+            if (w.seg == a.nseg - 1 && !ps.final) continue;
+            const float lam = a.lam.v[w.h];
+            const int dk = ps.dk, dv = ps.dv;
+            for (int t = w.t0; t < w.t_end; ++t, ++i) {
+                wait(&ctl, ctl.k, i, status);
+                if (i > 0) wait(&ctl, ctl.o, i - 1, status);         // decayed keys are free
+                const char *K = sm + K0 + (i & 1) * C::TILE;
+                if (ps.final) decay_keys<D, 3>(tid, K, sm, dk / 8, lam, end - 1 - t * T);
+                else decay_keys<D, 1>(tid, K, sm, dk / 8, lam, end - 1 - t * T);
+                fence_async_smem();
+                warp_arrive(&ctl.kd[i & 1]);
             }
-            if (row < dk && half * C::HALF + c < dv) put8(out + c, reinterpret_cast<const float *>(r));
+            const bool some = w.t0 < w.t_end;
+            const uint32_t acc = tm + ((uint32_t)(quarter * 32) << 16) + (done & 1) * (cols / 2) + half * C::HALF;
+            if (some) {
+                wait(&ctl, ctl.o, i - 1, status);
+                tc_fence_after_sync();
+            }
+            const size_t at = ((size_t)(w.b * a.H + w.h) * a.nseg + w.seg) * dk * dv + (size_t)row * dv + half * C::HALF;
+#pragma unroll 1
+            for (int c = 0; c < C::HALF; c += 8) {
+                uint32_t r[8] = {}, y[8] = {};
+                if (some) {
+                    ld8(acc + c, r);
+                    if (ps.final) ld8(acc + D + c, y);
+                    ld_wait();
+                }
+                if (row < dk && half * C::HALF + c < dv) {
+                    if (a.nseg > 1) put8(ps.local + at + c, reinterpret_cast<const float *>(r));
+                    if (ps.final) {
+                        float z[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) z[e] = f(r[e]) + f(y[e]);
+                        put8(ps.final + at + c, z);
+                    }
+                }
+            }
+            if (some) {
+                tc_fence_before_sync();
+                warp_arrive(&ctl.of[done & 1]);
+                ++done;
+            }
         }
-        tc_fence_before_sync();
     }
+    tc_fence_before_sync();
     __syncthreads();
     pdl_launch_dependents();
-    if (warp == 0) tmem_dealloc(tm, LC::COLS);
+    if (warp == 0) tmem_dealloc(tm, cols);
 }
 
 template <int D>
@@ -795,21 +848,23 @@ dig_status launch(const Args &a, bool local, cudaStream_t stream)
 {
     int *status = device_status_ptr();
     if (!status) return DIG_ERR_CUDA;
-    size_t smem = Cfg<D>::BYTES;
-    if (local) {
-        smem = 0;
-        for (int i = 0; i < a.passes; ++i) {
-            const size_t need = LocalCfg<D>::bytes(a.pass[i].x_end ? 3 : 1, a.pass[i].dk / 8);
-            smem = smem > need ? smem : need;
-        }
-    }
-    const void *fn = local ? (const void *)decay_local<D> : (const void *)decay_pass<D>;
-    const dig_status st = ensure_dynamic_smem(fn, smem);
-    if (st != DIG_OK) return st;
-    KernelTimer t(local ? KID_DECAY_LOCAL : KID_DECAY, stream);
     const long long items = (long long)a.nseg * a.passes * a.B * a.H;
-    if (local) return cuda_ok(launch_pdl(decay_local<D>, dim3((unsigned)items), dim3(LocalCfg<D>::THREADS), smem, stream, a, status));
-    return cuda_ok(launch_pdl(decay_pass<D>, dim3((unsigned)(items < kSms ? items : kSms)), dim3(kThreads), smem, stream, a, (int)items, status));
+    KernelTimer t(local ? KID_DECAY_LOCAL : KID_DECAY, stream);
+    if (!local) {
+        const dig_status st = ensure_dynamic_smem((const void *)decay_pass<D>, Cfg<D>::BYTES);
+        if (st != DIG_OK) return st;
+        return cuda_ok(launch_pdl(decay_pass<D>, dim3((unsigned)(items < kSms ? items : kSms)), dim3(kThreads), Cfg<D>::BYTES, stream, a, (int)items, status));
+    }
+    int parts = 1, most = 0;
+    for (int i = 0; i < a.passes; ++i) {
+        if (a.pass[i].final) parts = 3;
+        most = a.pass[i].dk > most ? a.pass[i].dk : most;
+    }
+    const size_t smem = LocalCfg<D>::bytes(parts, most / 8);
+    const dig_status st = ensure_dynamic_smem((const void *)decay_local<D>, smem);
+    if (st != DIG_OK) return st;
+    const long long room = (2 * (smem + 1024 + sizeof(Bars)) <= 228 * 1024 && 2 * LocalCfg<D>::cols(parts > 1) <= 512 ? 2ll : 1ll) * kSms;
+    return cuda_ok(launch_pdl(decay_local<D>, dim3((unsigned)(items < room ? items : room)), dim3(LocalCfg<D>::THREADS), smem, stream, a, (int)items, status));
 }
 
 }  // namespace
