@@ -183,6 +183,7 @@ dig_status run(Args &a, const Carved &w, int n, int end, int dtype, cudaStream_t
         if (!cut) l.pass[0] = last;
         dig_status st = pass_kernel(l, true, dtype, stream);
         if (st != DIG_OK) return st;
+        if (!cut && dtype == DIG_BF16) return pass_kernel(a, false, dtype, stream);          // the final state has been written
         // the scan: entering states of n passes, and the final one
         l.passes = cut ? n : 0;
         for (int i = 0; i < l.passes; ++i) l.pass[i].x_end = nullptr;

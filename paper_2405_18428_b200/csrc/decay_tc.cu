@@ -698,10 +698,12 @@ struct LocalCfg {
     // decayed keys first: their products read sixteen chunks from where a part starts, whatever stands there
     static constexpr int THREADS = 11 * 32;
     __host__ __device__ static constexpr int keys(int parts, int nch) { return (parts * nch * CH + 1023) / 1024 * 1024; }
-    static constexpr int bytes(int parts, int nch) { return keys(parts, nch) + 4 * Cfg<D>::TILE + 1024; }
+    // two buffers of decayed keys where they have three parts and there is room
+    __host__ __device__ static constexpr int bufs(int parts) { return parts > 1 && D <= 80 ? 2 : 1; }
+    static constexpr int bytes(int parts, int nch) { return bufs(parts) * keys(parts, nch) + 4 * Cfg<D>::TILE + 1024; }
     // tensor memory: two items' accumulators, of one part or of both
     __host__ __device__ static constexpr int cols(bool exact) { return exact ? (D <= 64 ? 256 : 512) : D <= 64 ? 128 : 256; }
-    static_assert(keys(3, Cfg<D>::NCH) + 4 * Cfg<D>::TILE + 1024 + sizeof(Bars) <= 227 * 1024, "fits");
+    static_assert(bufs(3) * keys(3, Cfg<D>::NCH) + 4 * Cfg<D>::TILE + 1024 + sizeof(Bars) <= 227 * 1024, "fits");
 };
 template <int D>
 __global__ void __launch_bounds__(LocalCfg<D>::THREADS, 2) decay_local(const __grid_constant__ Args a, int items, int *status)
@@ -718,7 +720,7 @@ __global__ void __launch_bounds__(LocalCfg<D>::THREADS, 2) decay_local(const __g
         any_final |= a.pass[j].final != nullptr;
         most = max(most, a.pass[j].dk);
     }
-    const int K0 = LC::keys(any_final ? 3 : 1, most / 8), V0 = K0 + 2 * C::TILE, cols = LC::cols(any_final);
+    const int parts = any_final ? 3 : 1, KB = LC::keys(parts, most / 8), bufs = LC::bufs(parts), K0 = bufs * KB, V0 = K0 + 2 * C::TILE, cols = LC::cols(any_final);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (warp == 0) tmem_alloc(&ctl.tmem, cols);
     if (tid == 32) {
@@ -776,11 +778,11 @@ __global__ void __launch_bounds__(LocalCfg<D>::THREADS, 2) decay_local(const __g
                 fence_async_smem();
                 tc_fence_after_sync();
                 if (elect_one()) {
-                    const uint32_t v = kd + V0 + (i & 1) * C::TILE;
-                    issue_state<D>(acc, kd, v, t > w.t0);
+                    const uint32_t v = kd + V0 + (i & 1) * C::TILE, keys = kd + (bufs == 2 ? (i & 1) * KB : 0);
+                    issue_state<D>(acc, keys, v, t > w.t0);
                     if (ps.final)
 #pragma unroll 1
-                        for (int j = 1; j < 3; ++j) issue_state<D>(acc + D, kd + j * part, v, t > w.t0 || j > 1);
+                        for (int j = 1; j < 3; ++j) issue_state<D>(acc + D, keys + j * part, v, t > w.t0 || j > 1);
                     mma_commit(&ctl.o[i & 1]);
                 }
                 __syncwarp();
@@ -798,10 +800,11 @@ __global__ void __launch_bounds__(LocalCfg<D>::THREADS, 2) decay_local(const __g
             const int dk = ps.dk, dv = ps.dv;
             for (int t = w.t0; t < w.t_end; ++t, ++i) {
                 wait(&ctl, ctl.k, i, status);
-                if (i > 0) wait(&ctl, ctl.o, i - 1, status);         // decayed keys are free
+                if (i >= bufs) wait(&ctl, ctl.o, i - bufs, status);  // decayed keys are free
                 const char *K = sm + K0 + (i & 1) * C::TILE;
-                if (ps.final) decay_keys<D, 3>(tid, K, sm, dk / 8, lam, end - 1 - t * T);
-                else decay_keys<D, 1>(tid, K, sm, dk / 8, lam, end - 1 - t * T);
+                char *to = sm + (bufs == 2 ? (i & 1) * KB : 0);
+                if (ps.final) decay_keys<D, 3>(tid, K, to, dk / 8, lam, end - 1 - t * T);
+                else decay_keys<D, 1>(tid, K, to, dk / 8, lam, end - 1 - t * T);
                 fence_async_smem();
                 warp_arrive(&ctl.kd[i & 1]);
             }
@@ -812,6 +815,10 @@ __global__ void __launch_bounds__(LocalCfg<D>::THREADS, 2) decay_local(const __g
                 tc_fence_after_sync();
             }
             const size_t at = ((size_t)(w.b * a.H + w.h) * a.nseg + w.seg) * dk * dv + (size_t)row * dv + half * C::HALF;
+            // an uncut sequence: the final state itself
+            const float *x0 = a.nseg == 1 ? ps.x0 : nullptr;
+            float *final = a.nseg == 1 ? ps.x_end : ps.final;
+            const float w0 = w.n > 0 ? exp2_of(lam * (w.n - 1 + ps.first + ps.last)) : 1.f, w1 = a.nseg == 1 && ps.last ? exp2_of(lam) : 1.f;
 #pragma unroll 1
             for (int c = 0; c < C::HALF; c += 8) {
                 uint32_t r[8] = {}, y[8] = {};
@@ -825,8 +832,11 @@ __global__ void __launch_bounds__(LocalCfg<D>::THREADS, 2) decay_local(const __g
                     if (ps.final) {
                         float z[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) z[e] = f(r[e]) + f(y[e]);
-                        put8(ps.final + at + c, z);
+                        for (int e = 0; e < 8; ++e) {
+                            z[e] = (f(r[e]) + f(y[e])) * w1;
+                            if (x0) z[e] = fmaf(w0, x0[at + c + e], z[e]);           // passes with a final state have theirs not transposed
+                        }
+                        put8(final + at + c, z);
                     }
                 }
             }
