@@ -310,7 +310,7 @@ dig_status dig_decay_step(const void *q, const void *k, const void *v, const flo
  *   strides: HOST array of the batch and token strides of q and k in elements, multiples of 16 bytes, or NULL: dense.
  *   positions: int32 [pos_batches][L][n_axes], DEVICE, pos_batches 1 or B; any values.
  *   freqs: HOST array of n_pairs values (radians per position); axes: HOST array of n_pairs values in 0 .. n_axes - 1.
- *   d: a multiple of 8, 8..128; d - 2 n_pairs a multiple of 4.  `dtype`: DIG_F32 or DIG_BF16.
+ *   H, H_k: at most 4096; d: a multiple of 8, 8..128; d - 2 n_pairs a multiple of 4.  `dtype`: DIG_F32 or DIG_BF16.
  * Angles are formed in 64 bits and reduced before they are rounded. */
 dig_status dig_rope(const void *q, const void *k, const long long *strides, const int *positions, int pos_batches, int n_axes,
                     const double *freqs, const int *axes, int n_pairs, void *q_out, void *k_out, int B, int L, int H, int H_k, int d,

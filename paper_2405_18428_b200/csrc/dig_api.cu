@@ -581,7 +581,7 @@ dig_status dig_rope(const void *q, const void *k, const long long *strides, cons
     if (!q || !positions || !freqs || !axes || !q_out || (k && !k_out) || (!k && k_out)) return DIG_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || (reinterpret_cast<uintptr_t>(positions) & 3u) != 0) return DIG_ERR_INVALID_ARG;
     if (B <= 0 || L <= 0 || H <= 0 || (k && H_k <= 0) || !valid_dim(d) || (dtype != DIG_F32 && dtype != DIG_BF16)) return DIG_ERR_INVALID_ARG;
-    if (H > 65535 || H_k > 65535 || (long long)B * L > 0x7fffffffll) return DIG_ERR_UNSUPPORTED;
+    if (H > 4096 || H_k > 4096 || (long long)B * L > 0x7fffffffll) return DIG_ERR_UNSUPPORTED;
     if ((pos_batches != 1 && pos_batches != B) || n_axes <= 0 || n_axes > 255 || n_pairs <= 0 || 2 * n_pairs > d || (d - 2 * n_pairs) % 4 != 0) return DIG_ERR_INVALID_ARG;
     if (!strides_ok(strides, k ? 4 : 2, dtype)) return DIG_ERR_INVALID_ARG;
     for (int i = 0; i < n_pairs; ++i)

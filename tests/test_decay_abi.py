@@ -76,7 +76,7 @@ def test_rope_refusals(L):
                 dict(H=0), dict(Hk=0), dict(d=12), dict(d=136), dict(dtype=2), dict(pb=3), dict(axes_n=0), dict(axes_n=1), dict(n=0), dict(n=5), dict(n=3), dict(freqs=nan),
                 dict(axes=(ctypes.c_int * 4)(0, -1, 1, 1)), dict(strides=(ctypes.c_longlong * 4)(8, 4, 8, 8))):
         assert rope(**bad) == dig.DIG_ERR_INVALID_ARG, bad
-    assert rope(B=1 << 20, pb=1, Lq=1 << 20) == rope(H=70000) == dig.DIG_ERR_UNSUPPORTED
+    assert rope(B=1 << 20, pb=1, Lq=1 << 20) == rope(H=4097) == rope(H=70000) == dig.DIG_ERR_UNSUPPORTED
 
 
 def test_rope_freqs():
