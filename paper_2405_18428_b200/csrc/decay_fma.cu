@@ -8,17 +8,20 @@ namespace {
 
 constexpr int T = kTileFma, NT = 256, LDP = T + 4;
 
-// Rows of a tile as fp32 in shared memory, stride d + 4 floats (a step of one row is a step of 4 banks); rows behind the end zero.
-__device__ __forceinline__ void load_rows(float *dst, const Args &a, const Rows &r, int d, int dir, int b, int h, int p0, int n)
+// Rows of a tile to shared memory, stride d + 4 floats (a step of one row is a step of 4 banks); rows behind the end zero.  Asynchronous:
+// loaded through registers, 16 bytes at a time, a tile's loads waited for memory four times over.
+__device__ __forceinline__ void load_rows(float *dst, const Rows &r, int d, int b, int h, const int (&tok)[4])
 {
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
     const float *base = (const float *)r.p + (size_t)b * r.batch + (size_t)(h / r.share) * d;
-    for (int i = threadIdx.x; i < T * (d / 4); i += NT) {
-        const int row = i / (d / 4), c = (i - row * (d / 4)) * 4, p = p0 + row;
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (p < n) x = load4(base + (size_t)token_at(a, dir, p, n) * r.token + c);
-        *reinterpret_cast<float4 *>(dst + row * (d + 4) + c) = x;
-    }
+    const uint32_t to = (uint32_t)__cvta_generic_to_shared(dst);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        for (int c = tx * 4; c < d; c += 64)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;"
+                         :: "r"(to + ((ty + 16 * i) * (d + 4) + c) * 4), "l"(base + (size_t)max(tok[i], 0) * r.token + c), "r"(tok[i] >= 0 ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void loads_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 __device__ __forceinline__ float dot4(float4 x, float4 y, float s) { return fmaf(x.x, y.x, fmaf(x.y, y.y, fmaf(x.z, y.z, fmaf(x.w, y.w, s)))); }
 __device__ __forceinline__ void axpy4(float4 &s, float w, float4 x)
@@ -26,6 +29,33 @@ __device__ __forceinline__ void axpy4(float4 &s, float w, float4 x)
     s.x = fmaf(w, x.x, s.x); s.y = fmaf(w, x.y, s.y); s.z = fmaf(w, x.z, s.z); s.w = fmaf(w, x.w, s.w);
 }
 __device__ __forceinline__ float4 scaled(float4 x, float w) { return make_float4(x.x * w, x.y * w, x.z * w, x.w * w); }
+
+// o[i] += rows ty + 16 i of A times B[..][c .. c + 3], over n (a multiple of 4) columns of A; LOWER: A is a lower triangle, of which what lies behind
+// a row is neither read as a factor nor, where it is NaN or infinite in B, spread.
+template <bool LOWER>
+__device__ __forceinline__ void rows4(float4 (&o)[4], const float *A, int lda, const float *B, int ldb, int ty, int c, int n)
+{
+#pragma unroll 1
+    for (int j = 0; j < n; j += 4) {
+        float4 p[4], x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            p[i] = *reinterpret_cast<const float4 *>(A + (ty + 16 * i) * lda + j);
+            x[i] = *reinterpret_cast<const float4 *>(B + (j + i) * ldb + c);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int last = ty + 16 * i;
+            if (!LOWER || j + 3 <= last) {
+                axpy4(o[i], p[i].x, x[0]); axpy4(o[i], p[i].y, x[1]); axpy4(o[i], p[i].z, x[2]); axpy4(o[i], p[i].w, x[3]);
+            } else if (j <= last) {
+                axpy4(o[i], p[i].x, x[0]);
+                if (j + 1 <= last) axpy4(o[i], p[i].y, x[1]);
+                if (j + 2 <= last) axpy4(o[i], p[i].z, x[2]);
+            }
+        }
+    }
+}
 
 template <bool LOCAL>
 __global__ void __launch_bounds__(NT) decay_fma(const __grid_constant__ Args a)
@@ -49,18 +79,28 @@ __global__ void __launch_bounds__(NT) decay_fma(const __grid_constant__ Args a)
     float *local = ps.local + ((size_t)bh * a.nseg + seg) * dd;
     const float *x0 = LOCAL ? nullptr : seg > 0 ? local : ps.x0 ? ps.x0 + (size_t)bh * dd : nullptr;
     const bool turned = seg > 0 ? ps.local_transposed : ps.x_transposed;
-    for (int i = tid; i < dk * dv; i += NT) {
-        const int r = i / dv, c = i - r * dv;
-        X[r * ldv + c] = x0 ? x0[turned ? c * dk + r : i] : 0.f;
+    if (x0 && turned) {
+        for (int c = ty; c < dv; c += 16)
+            for (int r = tx; r < dk; r += 16) X[r * ldv + c] = x0[c * dk + r];
+    } else {
+        for (int r = ty; r < dk; r += 16)
+            for (int c = tx * 4; c < dv; c += 64) *reinterpret_cast<float4 *>(X + r * ldv + c) = x0 ? load4(x0 + r * dv + c) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
     const int tiles = (a.L + T - 1) / T, t1 = min((seg + 1) * a.G, tiles);
     for (int t = seg * a.G; t < t1; ++t) {
         const int p0 = t * T, rows = min(T, n - p0), lead = p0 == 0 ? ps.first : 1;
         __syncthreads();
+        int tok[4];                              // of rows ty + 16 i
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int p = p0 + ty + 16 * i;
+            tok[i] = p < n ? scan_token(p, ps.dir, a.gh, a.gw, n) : -1;
+        }
         if (rows > 0) {
-            load_rows(K, a, ps.k, dk, ps.dir, b, h, p0, n);
-            load_rows(V, a, ps.v, dv, ps.dir, b, h, p0, n);
-            if (!LOCAL) load_rows(Q, a, ps.q, dk, ps.dir, b, h, p0, n);
+            load_rows(K, ps.k, dk, b, h, tok);
+            load_rows(V, ps.v, dv, b, h, tok);
+            if (!LOCAL) load_rows(Q, ps.q, dk, b, h, tok);
+            loads_done();
         }
         __syncthreads();
         if (!LOCAL) {
@@ -76,7 +116,7 @@ __global__ void __launch_bounds__(NT) decay_fma(const __grid_constant__ Args a)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) s[i][j] = dot4(qv[i], kv[j], s[i][j]);
+                        for (int j = 0; j <= i; ++j) s[i][j] = dot4(qv[i], kv[j], s[i][j]);           // blocks of 16 x 16 behind the diagonal are left out
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
@@ -87,28 +127,19 @@ __global__ void __launch_bounds__(NT) decay_fma(const __grid_constant__ Args a)
                     }
             }
             __syncthreads();
-            const size_t tok = (size_t)a.H * dv;
+            const size_t out = (size_t)a.H * dv;
             for (int c = tx * 4; c < dv; c += 64) {
                 float4 o[4] = {}, e[4] = {};
                 if (rows > 0) {
-                    // rows of one thread are 16 apart: nothing above the last of them counts
-                    for (int j = 0; j < T; ++j) {
-                        const float4 x = *reinterpret_cast<const float4 *>(V + j * ldv + c);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) if (j <= ty + 16 * i) axpy4(o[i], P[(ty + 16 * i) * LDP + j], x);
-                    }
-                    for (int j = 0; j < dk; ++j) {
-                        const float4 x = *reinterpret_cast<const float4 *>(X + j * ldv + c);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) axpy4(e[i], Q[(ty + 16 * i) * ldk + j], x);
-                    }
+                    rows4<true>(o, P, LDP, V, ldv, ty, c, T);
+                    rows4<false>(e, Q, ldk, X, ldv, ty, c, dk);
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int r = ty + 16 * i, p = p0 + r;
                     if (p >= a.L) continue;
                     if (p < n) axpy4(o[i], pw[r] * (lead ? pw[1] : 1.f), e[i]);
-                    const size_t at = ((size_t)b * a.L + token_at(a, ps.dir, p, n)) * tok + (size_t)h * dv + c;
+                    const size_t at = ((size_t)b * a.L + (p < n ? tok[i] : p)) * out + (size_t)h * dv + c;
                     const float4 y = p < n ? o[i] : make_float4(0.f, 0.f, 0.f, 0.f);
                     store4((float *)ps.out + at, y);
                 }
@@ -122,6 +153,7 @@ __global__ void __launch_bounds__(NT) decay_fma(const __grid_constant__ Args a)
                 float4 x[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[i] = scaled(*reinterpret_cast<const float4 *>(X + (r0 + i) * ldv + c), whole);
+#pragma unroll 4
                 for (int j = 0; j < rows; ++j) {
                     const float4 kv = scaled(*reinterpret_cast<const float4 *>(K + j * ldk + r0), pw[rows - 1 - j]);
                     const float4 vv = *reinterpret_cast<const float4 *>(V + j * ldv + c);
@@ -134,11 +166,12 @@ __global__ void __launch_bounds__(NT) decay_fma(const __grid_constant__ Args a)
     __syncthreads();
     if (LOCAL) {
         float *whole = ps.final ? ps.final + ((size_t)bh * a.nseg + seg) * dd : nullptr;
-        for (int i = tid; i < dk * dv; i += NT) {
-            const float x = X[i / dv * ldv + i % dv];
-            if (a.nseg > 1) local[i] = x;
-            if (whole) whole[i] = x;
-        }
+        for (int r = ty; r < dk; r += 16)
+            for (int c = tx * 4; c < dv; c += 64) {
+                const float4 x = *reinterpret_cast<const float4 *>(X + r * ldv + c);
+                if (a.nseg > 1) store4(local + r * dv + c, x);
+                if (whole) store4(whole + r * dv + c, x);
+            }
     }
     pdl_launch_dependents();
 }
