@@ -58,11 +58,6 @@ __device__ __forceinline__ int length_of(const int *lengths, int L, int b)
 {
     return lengths ? min(max(lengths[b], 0), L) : L;
 }
-// Token at scan position p of a sequence of n tokens; positions behind its end (row orders alone have them) are their own tokens.
-__device__ __forceinline__ int token_at(const Args &a, int dir, int p, int n)
-{
-    return p >= n ? p : scan_token(p, dir, a.gh, a.gw, n);
-}
 __device__ __forceinline__ float exp2_of(float x)
 {
     float y;
