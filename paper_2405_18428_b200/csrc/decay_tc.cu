@@ -41,15 +41,20 @@ template <int D>
 struct Cfg {
     static constexpr int PANELS = D / 64, REST = D % 64 / 16, TILE = PANELS * T * 128 + (REST ? 2 * CH + 992 : 0);
     static constexpr int NCH = D / 8, CHX = D * 16 + 16, XT = NCH * CHX, KEYS = NCH * CH;
-    static constexpr int STAGES = D == 128 ? 1 : 2, KEY_BUFS = STAGES, S_BUFS = STAGES;      // what shared and tensor memory hold
+    // What shared and tensor memory hold: tiles of q, k, v, and scores.  Wide heads have their keys decayed in place, which makes room for
+    // a second tile of them; with one tile of each, and keys apart, loads and decays took turns (80 sequences of 20 tiles: 112 us).
+    static constexpr bool IN_PLACE = D == 128;
+    static constexpr int Q_TILES = IN_PLACE ? 1 : 2, K_TILES = 2, V_TILES = Q_TILES, S_BUFS = Q_TILES;
+    // Who decays keys: the state's warps, or where they have the most to do the scores'.
+    static constexpr bool KEYS_BY_SCORE = D > 64;
     static constexpr int HALF = D / 2;                       // columns of a thread
     // tensor memory: scores (over them the decayed ones), outputs, what the entering state gives, the tile's own state
     static constexpr int S = 0, O = S_BUFS * 128, I = O + D, U = I + D;
     // shared memory: tiles, decayed keys, state (two parts), results
-    static constexpr int Q = 0, K = STAGES * TILE, V = 2 * STAGES * TILE, KD = 3 * STAGES * TILE, X = KD + KEY_BUFS * KEYS, R = X + 2 * XT;
+    static constexpr int Q = 0, K = Q_TILES * TILE, V = K + K_TILES * TILE, KD = V + V_TILES * TILE, X = KD + (IN_PLACE ? 0 : 2 * KEYS), R = X + 2 * XT;
     static constexpr int BYTES = R + KEYS + 1024;
     // a product reads sixteen chunks of decayed keys from where they start
-    static_assert(TILE % 1024 == 0 && U + D <= 512 && KD + (KEY_BUFS - 1) * KEYS + 16 * CH <= BYTES - 1024 && BYTES + 768 <= 227 * 1024, "fits");
+    static_assert(TILE % 1024 == 0 && U + D <= 512 && (IN_PLACE || KD + KEYS + 16 * CH <= BYTES - 1024) && BYTES + 768 <= 227 * 1024, "fits");
 };
 // Column of the decayed scores of keys 16 kk ..: the warps of keys 0 .. 31 and 64 .. 95 write over scores they have read themselves, and
 // so do those of the others.
@@ -250,17 +255,18 @@ __device__ __forceinline__ void value_step(uint32_t d, uint32_t v, int kk, F mma
     if constexpr (C::REST > 0) mma(d + C::PANELS * 64, mnmajor(v + C::PANELS * T * 128, CH) + kk * 16, idesc_bf16(128, 16, A_MN, true));
 }
 // U (+)= KD^T V: M = 128, rows beyond the keys' channels are whatever follows in shared memory and are not used.
-template <int D>
+template <int D, bool IN_PLACE = false>
 __device__ __forceinline__ void issue_state(uint32_t d, uint32_t kd, uint32_t v, bool accumulate)
 {
-    const uint64_t a = mnmajor(kd, CH);
+    const uint64_t a = IN_PLACE ? mnmajor_panel(kd) : mnmajor(kd, CH);
+    constexpr int step = IN_PLACE ? 128 : 16;
 #pragma unroll (D == 128 ? 1 : 8)
     for (int kk = 0; kk < T / 16; ++kk)
-        value_step<D, true>(d, v, kk, [&](uint32_t dd, uint64_t b, uint32_t idesc) { mma_f16(dd, a + kk * 16, b, idesc, accumulate || kk > 0); });
+        value_step<D, true>(d, v, kk, [&](uint32_t dd, uint64_t b, uint32_t idesc) { mma_f16(dd, a + kk * step, b, idesc, accumulate || kk > 0); });
 }
 
 // Decayed keys in PARTS parts of 8 bits: row j times g^(last - j).  Thread i of 256: one row, every second chunk.
-template <int D, int PARTS>
+template <int D, int PARTS, bool IN_PLACE = false>
 __device__ __forceinline__ void decay_keys(int i, const char *K, char *out, int nch, float lam, int last)
 {
     const int j = i & (T - 1);
@@ -281,7 +287,7 @@ __device__ __forceinline__ void decay_keys(int i, const char *K, char *out, int 
         }
 #pragma unroll
         for (int part = 0; part < PARTS; ++part)
-            *reinterpret_cast<uint4 *>(out + (part * nch + c) * CH + j * 16) = make_uint4(y[part][0], y[part][1], y[part][2], y[part][3]);
+            *reinterpret_cast<uint4 *>(out + (IN_PLACE ? chunk_at<D>(j, c) : (part * nch + c) * CH + j * 16)) = make_uint4(y[part][0], y[part][1], y[part][2], y[part][3]);
     }
 }
 // 8 columns of a row of results in fp32.
@@ -318,7 +324,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
     for (int j = 1; j < a.passes; ++j) alike &= a.pass[j].dk == a.pass[0].dk;
     const int odd = a.pass[0].dk & 8 ? a.pass[0].dk / 8 : 0;
     if (alike && odd) {
-        for (int j = tid; j < 2 * C::STAGES * T; j += kThreads) zero16(sm + j / T * C::TILE + chunk_at<D>(j % T, odd));
+        for (int j = tid; j < (C::Q_TILES + C::K_TILES) * T; j += kThreads) zero16(sm + j / T * C::TILE + chunk_at<D>(j % T, odd));
         fence_async_smem();
     }
     pdl_wait();
@@ -336,16 +342,14 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
             const Rows &r = which == 0 ? ps.q : which == 1 ? ps.k : ps.v;
             const int d = which == 2 ? ps.dv : ps.dk;
             for (int t = w.t0; t < w.t_end; ++t, ++i) {
-                const int old = i - C::STAGES;
-                if (old >= 0) {
+                const int tiles = which == 0 ? C::Q_TILES : which == 1 ? C::K_TILES : C::V_TILES, old = i - tiles;
+                if (old >= 0) {                  // its readers are done
                     if (which < 2) wait(&ctl, ctl.i, old, status);
                     if (which == 1) wait(&ctl, ctl.kd, old, status);
-                    if (which == 2) {
-                        wait(&ctl, ctl.u, old, status);
-                        wait(&ctl, ctl.o, old, status);
-                    }
+                    if (which == 2 || (which == 1 && C::IN_PLACE)) wait(&ctl, ctl.u, old, status);
+                    if (which == 2) wait(&ctl, ctl.o, old, status);
                 }
-                const uint32_t tile = (which * C::STAGES + i % C::STAGES) * C::TILE;
+                const uint32_t tile = (which == 0 ? C::Q : which == 1 ? C::K : C::V) + i % tiles * C::TILE;
                 uint64_t *bar = which == 0 ? &ctl.q[i & 1] : which == 1 ? &ctl.k[i & 1] : &ctl.v[i & 1];
                 load_tile<D>(a, base + tile, r, w, ps.dir, t, d);
                 if (alike) {
@@ -366,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
         auto scores = [&](int j, int ks) {       // of tile j
             tc_fence_after_sync();
             fence_async_smem();                  // q and k, as they have been waited for
-            const uint32_t q = base + C::Q + j % C::STAGES * C::TILE, k = base + C::K + j % C::STAGES * C::TILE, d = tm + C::S + j % C::S_BUFS * 128;
+            const uint32_t q = base + C::Q + j % C::Q_TILES * C::TILE, k = base + C::K + j % C::K_TILES * C::TILE, d = tm + C::S + j % C::S_BUFS * 128;
             if (elect_one()) {
                 each_channel_step<D>(q, ks, [&](int kk, uint64_t qa, uint32_t off) {
                     mma_f16(d, qa, C::REST > 0 && kk >= C::PANELS * 4 ? kmajor(k + C::PANELS * T * 128, CH) : kmajor_panel(k) + off, idesc_bf16(128, T, false, false), kk > 0);
@@ -383,25 +387,28 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
             const int ks = (ps.dk + 15) / 16;
             for (int t = w.t0; t < w.t_end; ++t, ++i) {
                 const bool next = t + 1 < w.t_end;
-                const uint32_t q = base + C::Q + i % C::STAGES * C::TILE, v = base + C::V + i % C::STAGES * C::TILE;
+                const uint32_t q = base + C::Q + i % C::Q_TILES * C::TILE, v = base + C::V + i % C::V_TILES * C::TILE;
                 if (ahead == i) {
                     if (C::S_BUFS == 1 && i > 0) wait(&ctl, ctl.o, i - 1, status);          // the decayed scores before are used up
                     wait(&ctl, ctl.q, i, status);
                     wait(&ctl, ctl.k, i, status);
                     scores(i, ks);
                 }
+                auto state = [&] {
+                    if (next) {
+                        wait(&ctl, ctl.kd, i, status);
+                        if (i > 0) wait(&ctl, ctl.uf, i - 1, status);
+                    }
+                    tc_fence_after_sync();
+                    if (elect_one()) {
+                        if (next) issue_state<D, C::IN_PLACE>(tm + C::U, C::IN_PLACE ? base + C::K + (i & 1) * C::TILE : base + C::KD + (i & 1) * C::KEYS, v, false);
+                        mma_commit(&ctl.u[i & 1]);
+                    }
+                    __syncwarp();
+                };
                 wait(&ctl, ctl.v, i, status);
                 fence_async_smem();
-                if (next) {
-                    wait(&ctl, ctl.kd, i, status);
-                    if (i > 0) wait(&ctl, ctl.uf, i - 1, status);
-                }
-                tc_fence_after_sync();
-                if (elect_one()) {
-                    if (next) issue_state<D>(tm + C::U, base + C::KD + i % C::KEY_BUFS * C::KEYS, v, false);
-                    mma_commit(&ctl.u[i & 1]);
-                }
-                __syncwarp();
+                if (!C::IN_PLACE) state();       // else the keys are decayed after the scores
                 wait(&ctl, ctl.x, i, status);
                 if (i > 0) wait(&ctl, ctl.of, i - 1, status);
                 tc_fence_after_sync();
@@ -431,6 +438,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
                     mma_commit(&ctl.o[i & 1]);
                 }
                 __syncwarp();
+                if (C::IN_PLACE) state();
             }
         }
     } else if (warp < kScore) {
@@ -465,9 +473,20 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
             }
             warp_arrive(&ctl.rf[j & 1]);
         };
+        auto keys = [&](const Item &w, int t, int j) {       // of the item's tile t, the list's tile j
+            wait(&ctl, ctl.k, j, status);
+            if (t + 1 < w.t_end) {
+                char *K = sm + C::K + (j & 1) * C::TILE;
+                if (!C::IN_PLACE && j >= 2) wait(&ctl, ctl.u, j - 2, status);        // what stood there has been used
+                decay_keys<D, 1, C::IN_PLACE>(tid, K, C::IN_PLACE ? K : sm + C::KD + (j & 1) * C::KEYS, a.pass[w.pass].dk / 8, a.lam.v[w.h], T - 1);
+                fence_async_smem();
+            }
+            warp_arrive(&ctl.kd[j & 1]);
+        };
         for (int item = blockIdx.x; item < items; item += gridDim.x) {
             const Item w = item_at(a, item);
             const float lam = a.lam.v[w.h];
+            if (C::KEYS_BY_SCORE && !C::IN_PLACE && w.t0 < w.t_end) keys(w, w.t0, i);
             // Factors of a block's 16 keys, g^(row - j0 - 15) and g^15 .. g^0.  Within the diagonal block the first goes up to g^-31, beyond
             // what fp32 holds where a position leaves less than 1/16: there the powers are formed one by one.
             const bool strong = lam < -4.f;
@@ -510,7 +529,9 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
                 tmem_st_wait();
                 tc_fence_before_sync();
                 warp_arrive(&ctl.p[i & 1]);
+                if (C::IN_PLACE) keys(w, t, i);  // the scores have them
                 if (i > 0) rows_out(i - 1);
+                if (C::KEYS_BY_SCORE && !C::IN_PLACE && t + 1 < w.t_end) keys(w, t + 1, i + 1);
             }
         }
         if (i > 0) rows_out(i - 1);
@@ -558,7 +579,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
             auto keys = [&](int t, int j) {      // of tile t, the list's tile j
                 wait(&ctl, ctl.k, j, status);
                 if (t + 1 < w.t_end) {
-                    decay_keys<D, 1>(me, sm + C::K + j % C::STAGES * C::TILE, sm + C::KD + j % C::KEY_BUFS * C::KEYS, dk / 8, lam, T - 1);
+                    decay_keys<D, 1>(me, sm + C::K + (j & 1) * C::TILE, sm + C::KD + (j & 1) * C::KEYS, dk / 8, lam, T - 1);
                     fence_async_smem();
                 }
                 warp_arrive(&ctl.kd[j & 1]);
@@ -582,10 +603,10 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
             if (i > 0) wait(&ctl, ctl.i, i - 1, status);             // the state before has been used
             if (x0) put_state(dk);
             warp_arrive(&ctl.x[i & 1]);
-            keys(w.t0, i);
+            if (!C::KEYS_BY_SCORE) keys(w.t0, i);
             for (int t = w.t0; t < w.t_end; ++t, ++i) {
                 const bool next = t + 1 < w.t_end;
-                if (C::KEY_BUFS == 2 && next) keys(t + 1, i + 1);
+                if (!C::KEYS_BY_SCORE && next) keys(t + 1, i + 1);
                 const float wn = exp2_of(lam * (T - 1 + (t == 0 ? ps.first : 1)));
                 wait(&ctl, ctl.u, i, status);
                 if (next && quarter * 32 < D) {
@@ -609,7 +630,6 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
                     wait(&ctl, ctl.i, i, status);
                     put_state(dk);
                     warp_arrive(&ctl.x[(i + 1) & 1]);
-                    if (C::KEY_BUFS == 1) keys(t + 1, i + 1);
                 }
             }
         }
