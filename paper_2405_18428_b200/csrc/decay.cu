@@ -194,16 +194,15 @@ dig_status run(Args &a, const Carved &w, int n, int end, int dtype, cudaStream_t
     a.nseg = w.plan.nseg; a.G = w.plan.G;
     Pass &last = a.pass[end];
     const bool cut = a.nseg > 1;
-    if (last.x_end) last.final = w.final;
+    if (last.x_end) last.final = w.final;            // uncut: not written, but says that the state is wanted
     if (cut || last.x_end) {
         Args l = a;
         l.passes = cut ? n : 1;
         if (!cut) l.pass[0] = last;
         dig_status st = pass_kernel(l, true, dtype, stream);
         if (st != DIG_OK) return st;
-        if (!cut && dtype == DIG_BF16) return pass_kernel(a, false, dtype, stream);          // the final state has been written
+        if (!cut) return pass_kernel(a, false, dtype, stream);           // the final state has been written
         // the scan: entering states of n passes, and the final one
-        l.passes = cut ? n : 0;
         for (int i = 0; i < l.passes; ++i) l.pass[i].x_end = nullptr;
         if (last.x_end) {
             l.pass[l.passes] = last;

@@ -165,12 +165,19 @@ __global__ void __launch_bounds__(NT) decay_fma(const __grid_constant__ Args a)
     }
     __syncthreads();
     if (LOCAL) {
-        float *whole = ps.final ? ps.final + ((size_t)bh * a.nseg + seg) * dd : nullptr;
+        // an uncut sequence: the final state itself, with the start state's part (passes with a final state have theirs not transposed)
+        float *whole = !ps.final ? nullptr : a.nseg == 1 ? ps.x_end + bh * dd : ps.final + ((size_t)bh * a.nseg + seg) * dd;
+        const float *start = a.nseg == 1 && ps.x0 ? ps.x0 + bh * dd : nullptr;
+        const float w0 = n > 0 ? exp2_of(lam * (n - 1 + ps.first + ps.last)) : 1.f, w1 = a.nseg == 1 && ps.last ? pw[1] : 1.f;
         for (int r = ty; r < dk; r += 16)
             for (int c = tx * 4; c < dv; c += 64) {
                 const float4 x = *reinterpret_cast<const float4 *>(X + r * ldv + c);
                 if (a.nseg > 1) store4(local + r * dv + c, x);
-                if (whole) store4(whole + r * dv + c, x);
+                if (whole) {
+                    float4 y = scaled(x, w1);
+                    if (start) axpy4(y, w0, load4(start + r * dv + c));
+                    store4(whole + r * dv + c, y);
+                }
             }
     }
     pdl_launch_dependents();
