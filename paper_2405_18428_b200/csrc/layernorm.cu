@@ -5,8 +5,9 @@
 // A CTA is as wide as a row and takes R rows at a time: their loads are on their way together, a turn ahead, the affine parameters and the sums of dw
 // and db stay in registers, and an exchange of sums between the warps serves all R rows.  Arithmetic on packed pairs: with one
 // multiply-add per value (and a row per warp, its parameters read again for every row) 16384 rows of 1152 in bf16 took 30 us forward,
-// 53 backward, bound by instructions.
+// 53 backward, bound by instructions; 21 and 29 us so (3.5 and 3.9 TB/s), bound by the turns' exchanges of sums and their barriers.
 #include <atomic>
+#include <type_traits>
 
 #include "dig_common.cuh"
 
@@ -35,6 +36,16 @@ template <> struct Raw<__nv_bfloat16, 8> {
         f[0] = bf2(in ? v.x : 0u); f[1] = bf2(in ? v.y : 0u); f[2] = bf2(in ? v.z : 0u); f[3] = bf2(in ? v.w : 0u);
     }
 };
+template <> struct Raw<float, 2> {
+    float2 v;
+    __device__ __forceinline__ void load(const float *p) { v = *reinterpret_cast<const float2 *>(p); }
+    __device__ __forceinline__ void unpack(float2 *f, bool in) const { f[0] = in ? v : make_float2(0.f, 0.f); }
+};
+template <> struct Raw<__nv_bfloat16, 2> {
+    uint32_t v;
+    __device__ __forceinline__ void load(const __nv_bfloat16 *p) { v = *reinterpret_cast<const uint32_t *>(p); }
+    __device__ __forceinline__ void unpack(float2 *f, bool in) const { f[0] = bf2(in ? v : 0u); }
+};
 template <typename T> struct Raw<T, 1> {
     T v;
     __device__ __forceinline__ void load(const T *p) { v = p[0]; }
@@ -44,6 +55,7 @@ template <int W>
 __device__ __forceinline__ void put(float *p, const float2 *f)
 {
     if constexpr (W == 1) p[0] = f[0].x;
+    else if constexpr (W == 2) *reinterpret_cast<float2 *>(p) = f[0];
     else {
 #pragma unroll
         for (int i = 0; i < W / 2; i += 2) store4(p + 2 * i, make_float4(f[i].x, f[i].y, f[i + 1].x, f[i + 1].y));
@@ -53,6 +65,7 @@ template <int W>
 __device__ __forceinline__ void put(__nv_bfloat16 *p, const float2 *f)
 {
     if constexpr (W == 1) p[0] = (__nv_bfloat16)f[0].x;
+    else if constexpr (W == 2) *reinterpret_cast<__nv_bfloat162 *>(p) = __floats2bfloat162_rn(f[0].x, f[0].y);
     else {
         uint4 u;
         uint32_t *o = &u.x;
@@ -69,6 +82,7 @@ template <int W>
 __device__ __forceinline__ void get_affine(const float *p, float2 *f)
 {
     if constexpr (W == 1) f[0] = make_float2(p[0], 0.f);
+    else if constexpr (W == 2) f[0] = *reinterpret_cast<const float2 *>(p);
     else {
 #pragma unroll
         for (int i = 0; i < W / 4; ++i) {
@@ -289,9 +303,9 @@ __global__ void __launch_bounds__(512) ln_bwd(const T *__restrict__ x, const T *
 #pragma unroll
         for (int q = 0; q < R; ++q) {
             if (j + q >= group_rows) break;
-            // dx = r (w dy) - r mean(g) - (x - mean) r^3 mean(g (x - mean))
+            // dx = r (w dy) - r mean(g) - (x - mean) r^3 mean(g (x - mean)); r^3 by itself overflows where eps is 1e-26 or less
             const float r = rsqrtf(over(s[q], n, inv) + eps);
-            const float2 r2 = both(r), shift = both(-r * mg[q]), slope = both(-r * r * r * (s[R + q] * inv));
+            const float2 r2 = both(r), shift = both(-r * mg[q]), slope = both(-r * (r * (r * (s[R + q] * inv))));
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const int c = (threadIdx.x + i * width) * W;
@@ -396,7 +410,9 @@ dig_status pick_fwd(const void *x, const float *w, const float *b, void *y, int 
     if (nv == 2) return go_fwd<T, W, 2>(x, w, b, y, groups, each, D, eps, s);
     if constexpr (W < 8) {
         if (nv == 4) return go_fwd<T, W, 4>(x, w, b, y, groups, each, D, eps, s);
-        if constexpr (W < 4) return nv == 8 ? go_fwd<T, W, 8>(x, w, b, y, groups, each, D, eps, s) : go_fwd<T, W, 16>(x, w, b, y, groups, each, D, eps, s);
+        if constexpr (W < 4)
+            if (nv == 8) return go_fwd<T, W, 8>(x, w, b, y, groups, each, D, eps, s);
+        if constexpr (W < 2) return go_fwd<T, W, 16>(x, w, b, y, groups, each, D, eps, s);
     }
     return DIG_ERR_UNSUPPORTED;
 }
@@ -426,18 +442,27 @@ dig_status pick_bwd(const void *x, const void *dy, const float *w, void *dx, flo
     if constexpr (W < 8) {
         if (nv == 4) return go_bwd<T, W, 4>(x, dy, w, dx, dw, db, part, ctas, groups, each, D, eps, s);
         if constexpr (W < 4)
-            return nv == 8 ? go_bwd<T, W, 8>(x, dy, w, dx, dw, db, part, ctas, groups, each, D, eps, s) : go_bwd<T, W, 16>(x, dy, w, dx, dw, db, part, ctas, groups, each, D, eps, s);
+            if (nv == 8) return go_bwd<T, W, 8>(x, dy, w, dx, dw, db, part, ctas, groups, each, D, eps, s);
+        if constexpr (W < 2) return go_bwd<T, W, 16>(x, dy, w, dx, dw, db, part, ctas, groups, each, D, eps, s);
     }
     return DIG_ERR_UNSUPPORTED;
 }
 
 }  // namespace
 
+// The widest access that rows of D values allow: 16 bytes, two values, or one.  16384 rows in bf16, forward / backward: 1152 values by
+// eights 21 / 29 us, 1002 by twos 46 / 66 (one by one 56 / 108), 1001 one by one 56 / 111.
+template <typename F>
+dig_status with_width(int D, int dtype, F go)
+{
+    using bf16 = __nv_bfloat16;
+    if (dtype == DIG_F32) return D % 4 == 0 ? go(float(), std::integral_constant<int, 4>()) : D % 2 == 0 ? go(float(), std::integral_constant<int, 2>()) : go(float(), std::integral_constant<int, 1>());
+    return D % 8 == 0 ? go(bf16(), std::integral_constant<int, 8>()) : D % 2 == 0 ? go(bf16(), std::integral_constant<int, 2>()) : go(bf16(), std::integral_constant<int, 1>());
+}
+
 dig_status launch_layernorm_fwd(const void *x, const float *w, const float *b, void *y, long long rows, int groups, int D, float eps, int dtype, cudaStream_t s)
 {
-    const long long each = rows / groups;
-    if (dtype == DIG_F32) return D % 4 == 0 ? pick_fwd<float, 4>(x, w, b, y, groups, each, D, eps, s) : pick_fwd<float, 1>(x, w, b, y, groups, each, D, eps, s);
-    return D % 8 == 0 ? pick_fwd<__nv_bfloat16, 8>(x, w, b, y, groups, each, D, eps, s) : pick_fwd<__nv_bfloat16, 1>(x, w, b, y, groups, each, D, eps, s);
+    return with_width(D, dtype, [&](auto t, auto width) { return pick_fwd<decltype(t), decltype(width)::value>(x, w, b, y, groups, rows / groups, D, eps, s); });
 }
 
 size_t layernorm_bwd_workspace_bytes(long long rows, int groups, int D)
@@ -450,10 +475,8 @@ dig_status launch_layernorm_bwd(const void *x, const void *dy, const float *w, v
 {
     const long long each = rows / groups;
     const int ctas = bwd_ctas(each, groups, D);
-    const dig_status st = dtype == DIG_F32 ? (D % 4 == 0 ? pick_bwd<float, 4>(x, dy, w, dx, dw, db, part, ctas, groups, each, D, eps, s)
-                                                         : pick_bwd<float, 1>(x, dy, w, dx, dw, db, part, ctas, groups, each, D, eps, s))
-                                           : (D % 8 == 0 ? pick_bwd<__nv_bfloat16, 8>(x, dy, w, dx, dw, db, part, ctas, groups, each, D, eps, s)
-                                                         : pick_bwd<__nv_bfloat16, 1>(x, dy, w, dx, dw, db, part, ctas, groups, each, D, eps, s));
+    const dig_status st =
+        with_width(D, dtype, [&](auto t, auto width) { return pick_bwd<decltype(t), decltype(width)::value>(x, dy, w, dx, dw, db, part, ctas, groups, each, D, eps, s); });
     if (st != DIG_OK || (!dw && !db) || ctas == 1) return st;
     KernelTimer t(KID_LN_SUM, s);
     if (ctas <= 16) return cuda_ok(launch_pdl(ln_sum<true>, dim3((2 * D + 255) / 256, groups), dim3(256), 0, s, (const float *)part, dw, db, ctas, D));

@@ -42,6 +42,7 @@ def check(B, H, Hk, gh, gw, dk, dv, dtype, direction, *, log_decay=None, state=F
     for name, a, b, m in zip(("dq", "dk", "dv"), got, want, size):
         ref.close(name, a, b, m, dtype, terms * (H // Hk))
     ref.close("ds_in", got[3], want[3], size[3], dtype, terms, state=True)
+    assert dig.dig_last_device_status() == dig.DIG_OK
     again = dig.dig_decay_bwd(q, k, v, log_decay, d_out, gh, gw, direction, s_in=s_in, ds_out=ds_out, lengths=n)
     assert again[3] is None and all(torch.equal(a, b) for a, b in zip(again[:3], got[:3]))
 

@@ -52,7 +52,7 @@ def check(rows, D, groups, dtype, *, affine=True, seed=0, eps=1e-5, offset=1.0):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("D", [1, 2, 7, 8, 33, 64, 255, 256, 384, 520, 768, 1001, 1024, 1152, 2048, 2056, 4095, 4096, 5000, 8191, 8192])
+@pytest.mark.parametrize("D", [1, 2, 7, 8, 33, 64, 255, 256, 384, 520, 766, 768, 1001, 1002, 1024, 1152, 2048, 2056, 4094, 4095, 4096, 5000, 6002, 8191, 8192])
 def test_row_lengths(dtype, D):
     check(37, D, 1, dtype, seed=D)
 
@@ -76,6 +76,17 @@ def test_constant_rows_give_the_bias_and_no_infinity():
     assert torch.equal(dig.dig_layernorm_fwd(x, None, b), b.expand(4, -1))
     dx, dw, db = dig.dig_layernorm_bwd(x, torch.ones_like(x))
     assert torch.isfinite(dx).all() and (dw == 0).all() and (db == 4).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_constant_rows_and_a_small_eps(dtype):
+    from paper_2405_18428_b200 import dig
+    x, dy = torch.full((4, 384), 3.0, device="cuda", dtype=dtype), torch.zeros(4, 384, device="cuda", dtype=dtype)
+    dy[:, 0], dy[:, 1] = 1, -1                               # mean(g) = 0: dx = r dy, and r = 2^50
+    dx, dw, db = dig.dig_layernorm_bwd(x, dy, None, 2.0 ** -100)
+    # 1 / sqrt(eps) to two units in the last place of fp32, and a rounding to the type
+    assert ((dx.double() - dy.double() * 2.0 ** 50).abs() <= 2.0 ** 50 * (torch.finfo(dtype).eps / 2 + 2.0 ** -22) * dy.double().abs()).all()
+    assert (dw == 0).all() and torch.equal(db, 4 * dy[0].float())
 
 
 def test_a_nan_stays_in_its_row():
