@@ -31,8 +31,8 @@ struct Plan {
 // How many segments.  Costs in tiles of the pass: a round of segments on all CTAs that run together takes its tiles and a fill; a cut
 // adds the local pass (of the states that enter segments: one pass of them forward, two backward), its launches, and the scan over all segments.
 // Fitted to 2283 measured calls of 6 to 480 sequences of 2 to 128 tiles, 1 to 64 segments, heads of 64, 72 and 128 channels: the cut chosen
-// is 0.05% off the best on average in bf16 (worst 6%), 1% in fp32 (worst 17%); 4% off for forward passes that return the final state, whose
-// results are to be the same.
+// is 0.15% off the best on average in bf16 (worst 12%), 1.2% in fp32 (worst 18%); forward passes that return the final state, 3% (worst 37%:
+// results are not to depend on whether it is asked for).
 struct Cost {
     int slots;                           // CTAs on an SM: of the pass,
     int local_slots;                     // of the local pass

@@ -344,7 +344,9 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
             for (int t = w.t0; t < w.t_end; ++t, ++i) {
                 const int tiles = which == 0 ? C::Q_TILES : which == 1 ? C::K_TILES : C::V_TILES, old = i - tiles;
                 if (old >= 0) {                  // its readers are done
-                    if (which < 2) wait(&ctl, ctl.i, old, status);
+                    // keys are free after the scores and their decays; where the scores' warps decay them, loading that early takes 1% longer
+                    if (which == 1 && !C::KEYS_BY_SCORE) wait(&ctl, ctl.s, old, status);
+                    else if (which < 2) wait(&ctl, ctl.i, old, status);
                     if (which == 1) wait(&ctl, ctl.kd, old, status);
                     if (which == 2 || (which == 1 && C::IN_PLACE)) wait(&ctl, ctl.u, old, status);
                     if (which == 2) wait(&ctl, ctl.o, old, status);
@@ -406,9 +408,14 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
                     }
                     __syncwarp();
                 };
-                wait(&ctl, ctl.v, i, status);
-                fence_async_smem();
-                if (!C::IN_PLACE) state();       // else the keys are decayed after the scores
+                auto values = [&] {
+                    wait(&ctl, ctl.v, i, status);
+                    fence_async_smem();
+                };
+                if (!C::IN_PLACE) {
+                    values();
+                    state();
+                }
                 wait(&ctl, ctl.x, i, status);
                 if (i > 0) wait(&ctl, ctl.of, i - 1, status);
                 tc_fence_after_sync();
@@ -426,6 +433,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
                 // The next tile's scores, where they need not be waited for.  The decayed scores that they take the place of were used up before
                 // the results that the wait above was for.
                 if (C::S_BUFS == 2 && next && ready(ctl.q, i + 1) && ready(ctl.k, i + 1)) scores(i + 1, ks);
+                if (C::IN_PLACE) values();       // the product before lets go of q
                 wait(&ctl, ctl.p, i, status);
                 tc_fence_after_sync();
                 if (elect_one()) {
@@ -438,7 +446,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
                     mma_commit(&ctl.o[i & 1]);
                 }
                 __syncwarp();
-                if (C::IN_PLACE) state();
+                if (C::IN_PLACE) state();        // the keys are decayed after the scores
             }
         }
     } else if (warp < kScore) {
