@@ -1,5 +1,7 @@
 // Linear attention with a decay for each head: cuts, workspace, the scan that joins segments, the sum over heads that share
 // keys and values, and the single-token form.  Equations in decay.cuh.
+#include <algorithm>
+
 #include "decay_plan.cuh"
 
 namespace dig {
@@ -43,20 +45,36 @@ __global__ void __launch_bounds__(256) decay_scan(const __grid_constant__ ScanAr
     if (ps.x_end) ps.x_end[(size_t)bh * dd + e] = n > 0 && ps.last ? x * exp2_of(lam) : x;         // no token: the start state
 }
 
-// out[t][hk] = sum over the heads that share hk, in their order.
+// out[t][hk] = sum over the heads that share hk, in their order; of dk and dv (blockIdx.y).  Bound by the bytes of the partial gradients.
+struct ShareArgs {
+    const float *part[2];
+    void *out[2];
+    int d4[2];
+    long long rows;                      // tokens times shared heads
+    int share;
+};
 template <typename S>
-__global__ void __launch_bounds__(256) share_sum(const float *__restrict__ part, S *__restrict__ out, size_t n4, int share, int d4)
+__global__ void __launch_bounds__(256) share_sum(const __grid_constant__ ShareArgs a)
 {
     pdl_wait();
     pdl_launch_dependents();
-    const size_t step = (size_t)gridDim.x * 256;
+    const int d4 = a.d4[blockIdx.y], share = a.share;
+    const float *part = a.part[blockIdx.y];
+    S *out = (S *)a.out[blockIdx.y];
+    const size_t step = (size_t)gridDim.x * 256, n4 = (size_t)a.rows * d4;
     for (size_t i = blockIdx.x * (size_t)256 + threadIdx.x; i < n4; i += step) {
-        const size_t row = i / d4;                   // (token, shared head)
+        const size_t row = i / d4;
         const float *p = part + (row * share * d4 + (i - row * d4)) * 4;
-        float4 s = load4(p);
-        for (int g = 1; g < share; ++g) {
-            const float4 x = load4(p + (size_t)g * d4 * 4);
-            s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int g = 0; g < share; g += 4) {                     // four are asked for together
+            float4 x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = load4(p + (size_t)min(g + e, share - 1) * d4 * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (g + e >= share) break;
+                s.x += x[e].x; s.y += x[e].y; s.z += x[e].z; s.w += x[e].w;
+            }
         }
         store4(out + i * 4, s);
     }
@@ -78,13 +96,12 @@ dig_status launch_scan(const Args &a, int tile, cudaStream_t stream)
     return cuda_ok(launch_pdl(decay_scan, dim3((most + 255) / 256, a.B * a.H, a.passes), dim3(256), 0, stream, s));
 }
 
-dig_status launch_share_sum(const float *part, void *out, long long rows, int H, int share, int d, int dtype, cudaStream_t stream)
+dig_status launch_share_sum(const ShareArgs &a, int dtype, cudaStream_t stream)
 {
-    const size_t n4 = (size_t)rows * (H / share) * (d / 4), blocks = (n4 + 255) / 256, most = (size_t)kSms * 8;
-    const dim3 grid((unsigned)(blocks < most ? blocks : most));
+    const size_t blocks = ((size_t)a.rows * std::max(a.d4[0], a.d4[1]) + 255) / 256, most = (size_t)kSms * 8;
+    const dim3 grid((unsigned)std::min(blocks, most), 2);
     KernelTimer t(KID_DECAY_SUM, stream);
-    if (dtype == DIG_F32) return cuda_ok(launch_pdl(share_sum<float>, grid, dim3(256), 0, stream, part, (float *)out, n4, share, d / 4));
-    return cuda_ok(launch_pdl(share_sum<__nv_bfloat16>, grid, dim3(256), 0, stream, part, (__nv_bfloat16 *)out, n4, share, d / 4));
+    return cuda_ok(dtype == DIG_F32 ? launch_pdl(share_sum<float>, grid, dim3(256), 0, stream, a) : launch_pdl(share_sum<__nv_bfloat16>, grid, dim3(256), 0, stream, a));
 }
 
 // ---- one token ------------------------------------------------------------------------------------------------------
@@ -257,8 +274,10 @@ dig_status decay_bwd_launch(const DecayCall &c)
     dk.local_transposed = 1; dk.dk = c.dv; dk.dv = c.dk; dk.dir = c.dir ^ 1; dk.out_f32 = share > 1;
     dig_status st = run(a, w, 2, 1, c.dtype, c.stream);
     if (st != DIG_OK || share == 1) return st;
-    st = launch_share_sum(w.part_k, c.dk_out, (long long)c.B * c.L, c.H, share, c.dk, c.dtype, c.stream);
-    return st != DIG_OK ? st : launch_share_sum(w.part_v, c.dv_out, (long long)c.B * c.L, c.H, share, c.dv, c.dtype, c.stream);
+    ShareArgs sum{};
+    sum.part[0] = w.part_k; sum.part[1] = w.part_v; sum.out[0] = c.dk_out; sum.out[1] = c.dv_out;
+    sum.d4[0] = c.dk / 4; sum.d4[1] = c.dv / 4; sum.rows = (long long)c.B * c.L * c.H_kv; sum.share = share;
+    return launch_share_sum(sum, c.dtype, c.stream);
 }
 
 }  // namespace dig

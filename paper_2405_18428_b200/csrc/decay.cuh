@@ -65,10 +65,8 @@ __device__ __forceinline__ float exp2_of(float x)
     return y;
 }
 
-// Joins segments: kernel of decay_scan.cu.
+// Joins segments: kernel of decay.cu.
 dig_status launch_scan(const Args &a, int tile, cudaStream_t stream);
-// Sums the partial gradients of heads that share keys and values.
-dig_status launch_share_sum(const float *part, void *out, long long rows, int H, int share, int d, int dtype, cudaStream_t stream);
 
 // Rows of a tile, and the two kinds of kernels.
 constexpr int kTileFma = 64, kTileTc = 128;
