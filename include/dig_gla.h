@@ -279,7 +279,8 @@ dig_status dig_gla_bwd_multi(const void *q, const void *k, const void *v, const 
  *   log_decay_per_head: HOST array of H finite values <= 0.
  *   lengths: [B] tokens of each sequence, DEVICE, or NULL for L each; values outside 0..L count as the nearest of the two.  Rows of
  *   out behind the end of a sequence are zeros, what q, k and v hold there is not used.  Row orders only (else DIG_ERR_UNSUPPORTED).
- *   s_in: state before the first token, fp32 [B][H][d_k][d_v], NULL = 0; s_out: receives the state after the last token, or NULL.
+ *   s_in: state before the first token, fp32 [B][H][d_k][d_v], NULL = 0; s_out: receives the state after the last token, or NULL; not
+ *   the same array (DIG_ERR_INVALID_ARG).
  * fp32 storage: fp32 FMA arithmetic.  bf16 storage: q, k and v enter the products as they are, decayed scores, states and (for out) decayed
  * keys as bf16, sums in fp32; s_out is summed apart with decayed keys of 24 bits and has fp32 accuracy.
  * A NaN or an infinity in v reaches rows of the same 32 positions before it (products with zeros), never earlier ones. */
@@ -291,7 +292,7 @@ dig_status dig_decay_fwd(const void *q, const void *k, const void *v, const long
 
 /* Reverse mode of dig_decay_fwd: gradients of <d_out, out> + <ds_out, s_out> (NULL ds_out = 0).  Nothing is saved by the forward call.
  *   d_out: [B][L][H][d_v], dense; dq: [B][L][H][d_k]; dk: [B][L][H_kv][d_k]; dv: [B][L][H_kv][d_v], summed over the heads that share them;
- *   ds_in: gradient with respect to s_in, or NULL.  Rows behind the end of a sequence are zeros.  The decays get no gradient. */
+ *   ds_in: gradient with respect to s_in, or NULL; neither s_in nor ds_out themselves.  Rows behind the end of a sequence are zeros.  The decays get no gradient. */
 dig_status dig_decay_bwd(const void *q, const void *k, const void *v, const long long *strides, const float *log_decay_per_head,
                          const int *lengths, const void *d_out, const float *s_in, const float *ds_out, void *dq, void *dk, void *dv,
                          float *ds_in, int B, int H, int H_kv, int grid_h, int grid_w, int d_k, int d_v, int direction, int dtype,

@@ -205,30 +205,34 @@ Rows rows_of(const void *p, const long long *strides, long long L, int heads, in
 }
 
 // Local pass and scan for the states that enter segments, where the sequences are cut (of the passes that have states of their own, the
-// first `n`), and for the state that the caller wants (of the pass `end`), then the passes themselves.
+// first `n`), then the passes themselves.  The state that the caller wants (of the pass `end`): the fp32 kernels' last segments end with it;
+// the tensor-core kernels sum it apart, in the local pass.
 dig_status run(Args &a, const Carved &w, int n, int end, int dtype, cudaStream_t stream)
 {
     a.nseg = w.plan.nseg; a.G = w.plan.G;
     Pass &last = a.pass[end];
-    const bool cut = a.nseg > 1;
-    if (last.x_end) last.final = w.final;            // uncut: not written, but says that the state is wanted
-    if (cut || last.x_end) {
-        Args l = a;
-        l.passes = cut ? n : 1;
-        if (!cut) l.pass[0] = last;
+    const bool cut = a.nseg > 1, apart = last.x_end && dtype != DIG_F32;
+    if (apart) last.final = w.final;                 // uncut: not written, but says that the state is wanted
+    Args l = a;
+    if (cut) {
+        l.passes = n;
         dig_status st = pass_kernel(l, true, dtype, stream);
         if (st != DIG_OK) return st;
-        if (!cut) return pass_kernel(a, false, dtype, stream);           // the final state has been written
         // the scan: entering states of n passes, and the final one
-        for (int i = 0; i < l.passes; ++i) l.pass[i].x_end = nullptr;
-        if (last.x_end) {
-            l.pass[l.passes] = last;
+        for (int i = 0; i < n; ++i) l.pass[i].x_end = nullptr;
+        if (apart) {
+            l.pass[n] = last;
             l.pass[l.passes++].local = w.final;
         }
         st = launch_scan(l, w.plan.tile, stream);
-        if (st != DIG_OK) return st;
+        return st != DIG_OK ? st : pass_kernel(a, false, dtype, stream);
     }
-    return pass_kernel(a, false, dtype, stream);
+    a.beside = l.beside = apart;
+    const dig_status st = pass_kernel(a, false, dtype, stream);
+    if (st != DIG_OK || !apart) return st;
+    l.passes = 1;
+    l.pass[0] = last;
+    return pass_kernel(l, true, dtype, stream);
 }
 
 // The tensor-core kernels count results in 16 bytes with 32 bits.

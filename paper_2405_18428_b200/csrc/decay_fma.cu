@@ -60,7 +60,7 @@ __device__ __forceinline__ void rows4(float4 (&o)[4], const float *A, int lda, c
 template <bool LOCAL>
 __global__ void __launch_bounds__(NT) decay_fma(const __grid_constant__ Args a)
 {
-    if (LOCAL && blockIdx.x == a.nseg - 1 && !a.pass[blockIdx.z].final) {            // goes into the final state only
+    if (LOCAL && blockIdx.x == a.nseg - 1) {                     // enters no segment
         pdl_wait();
         pdl_launch_dependents();
         return;
@@ -87,6 +87,7 @@ __global__ void __launch_bounds__(NT) decay_fma(const __grid_constant__ Args a)
             for (int c = tx * 4; c < dv; c += 64) *reinterpret_cast<float4 *>(X + r * ldv + c) = x0 ? load4(x0 + r * dv + c) : make_float4(0.f, 0.f, 0.f, 0.f);
     }
     const int tiles = (a.L + T - 1) / T, t1 = min((seg + 1) * a.G, tiles);
+    float *end = !LOCAL && ps.x_end && seg == a.nseg - 1 ? ps.x_end + bh * dd : nullptr;         // the final state is wanted, and this is the last segment
     for (int t = seg * a.G; t < t1; ++t) {
         const int p0 = t * T, rows = min(T, n - p0), lead = p0 == 0 ? ps.first : 1;
         __syncthreads();
@@ -146,7 +147,7 @@ __global__ void __launch_bounds__(NT) decay_fma(const __grid_constant__ Args a)
             }
             __syncthreads();
         }
-        if (rows <= 0) continue;
+        if (rows <= 0 || (!LOCAL && t + 1 == t1 && !end)) continue;
         const float whole = pw[rows - 1] * (lead ? pw[1] : 1.f);
         for (int r0 = ty * 4; r0 < dk; r0 += 64)
             for (int c = tx * 4; c < dv; c += 64) {
@@ -164,21 +165,10 @@ __global__ void __launch_bounds__(NT) decay_fma(const __grid_constant__ Args a)
             }
     }
     __syncthreads();
-    if (LOCAL) {
-        // an uncut sequence: the final state itself, with the start state's part (passes with a final state have theirs not transposed)
-        float *whole = !ps.final ? nullptr : a.nseg == 1 ? ps.x_end + bh * dd : ps.final + ((size_t)bh * a.nseg + seg) * dd;
-        const float *start = a.nseg == 1 && ps.x0 ? ps.x0 + bh * dd : nullptr;
-        const float w0 = n > 0 ? exp2_of(lam * (n - 1 + ps.first + ps.last)) : 1.f, w1 = a.nseg == 1 && ps.last ? pw[1] : 1.f;
+    if (LOCAL || end) {
+        const float w = end && ps.last && n > 0 ? pw[1] : 1.f;
         for (int r = ty; r < dk; r += 16)
-            for (int c = tx * 4; c < dv; c += 64) {
-                const float4 x = *reinterpret_cast<const float4 *>(X + r * ldv + c);
-                if (a.nseg > 1) store4(local + r * dv + c, x);
-                if (whole) {
-                    float4 y = scaled(x, w1);
-                    if (start) axpy4(y, w0, load4(start + r * dv + c));
-                    store4(whole + r * dv + c, y);
-                }
-            }
+            for (int c = tx * 4; c < dv; c += 64) store4((LOCAL ? local : end) + r * dv + c, scaled(*reinterpret_cast<const float4 *>(X + r * ldv + c), w));
     }
     pdl_launch_dependents();
 }

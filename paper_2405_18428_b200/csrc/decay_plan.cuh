@@ -65,7 +65,7 @@ inline Plan make_plan(int B, int H, int L, bool backward, int d, int dtype)
 }
 
 // Workspace, every block 256-byte aligned: where sequences are cut states of the segments, [B*H][nseg][dk][dv] fp32 (backward: of two
-// passes), the same once more for the final state, and where heads share keys and values the gradients of each head before they are summed, fp32 [B][L][H][d].
+// passes), the same once more for the final state of bf16 calls, and where heads share keys and values the gradients of each head before they are summed, fp32 [B][L][H][d].
 struct Carved {
     Plan plan;
     float *local[2], *final, *part_k, *part_v;
@@ -79,7 +79,7 @@ inline Carved carve(char *base, int B, int H, int H_kv, int L, int dk, int dv, i
     auto take = [&](size_t bytes) { char *p = base + o; o += align256(bytes); return reinterpret_cast<float *>(p); };
     const size_t state = w.plan.nseg > 1 ? (size_t)B * H * w.plan.nseg * dk * dv * 4 : 16;
     w.local[0] = take(state);
-    w.final = take(state);
+    w.final = take(dtype == DIG_F32 ? 0 : state);
     if (backward) {
         w.local[1] = take(state);
         if (H != H_kv) {

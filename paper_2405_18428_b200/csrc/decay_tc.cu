@@ -328,6 +328,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
         fence_async_smem();
     }
     pdl_wait();
+    if (a.beside) pdl_launch_dependents();
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
@@ -759,7 +760,7 @@ __global__ void __launch_bounds__(LocalCfg<D>::THREADS, 2) decay_local(const __g
         ctl.dead = 0;
         fence_barrier_init();
     }
-    pdl_wait();
+    if (!a.beside) pdl_wait();
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
@@ -862,7 +863,7 @@ __global__ void __launch_bounds__(LocalCfg<D>::THREADS, 2) decay_local(const __g
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
                             z[e] = (f(r[e]) + f(y[e])) * w1;
-                            if (x0) z[e] = fmaf(w0, x0[at + c + e], z[e]);           // passes with a final state have theirs not transposed
+                            if (x0) z[e] = fmaf(w0, __ldcg(x0 + at + c + e), z[e]);           // passes with a final state have theirs not transposed
                         }
                         put8(final + at + c, z);
                     }
@@ -879,6 +880,7 @@ __global__ void __launch_bounds__(LocalCfg<D>::THREADS, 2) decay_local(const __g
     __syncthreads();
     pdl_launch_dependents();
     if (warp == 0) tmem_dealloc(tm, cols);
+    if (a.beside && blockIdx.x == 0) pdl_wait();             // complete only after the passes; the other CTAs make room
 }
 
 template <int D>

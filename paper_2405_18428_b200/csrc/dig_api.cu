@@ -535,6 +535,7 @@ dig_status dig_decay_fwd(const void *q, const void *k, const void *v, const long
     if (!decay_geometry_ok(B, H, H_kv, grid_h, grid_w, d_k, d_v, dtype) || direction < 0 || direction > 3) return DIG_ERR_INVALID_ARG;
     if (!strides_ok(strides, 6, dtype) || (reinterpret_cast<uintptr_t>(lengths) & 3u) != 0) return DIG_ERR_INVALID_ARG;
     if (lengths && (direction & 2)) return DIG_ERR_UNSUPPORTED;
+    if (s_out && s_out == s_in) return DIG_ERR_INVALID_ARG;                        // the start is read while the result is written
     if (!workspace || !aligned16(workspace) || workspace_bytes < decay_workspace_bytes(B, H, H_kv, grid_h * grid_w, d_k, d_v, dtype, false)) return DIG_ERR_WORKSPACE;
     DecayCall c{};
     c.q = q; c.k = k; c.v = v; c.strides = strides; c.log_decay = log_decay_per_head; c.lengths = lengths; c.s_in = s_in; c.out = out; c.s_out = s_out;
@@ -555,6 +556,7 @@ dig_status dig_decay_bwd(const void *q, const void *k, const void *v, const long
     if (!decay_geometry_ok(B, H, H_kv, grid_h, grid_w, d_k, d_v, dtype) || direction < 0 || direction > 3) return DIG_ERR_INVALID_ARG;
     if (!strides_ok(strides, 6, dtype) || (reinterpret_cast<uintptr_t>(lengths) & 3u) != 0) return DIG_ERR_INVALID_ARG;
     if (lengths && (direction & 2)) return DIG_ERR_UNSUPPORTED;
+    if (ds_in && (ds_in == s_in || ds_in == ds_out)) return DIG_ERR_INVALID_ARG;                        // the start is read while the result is written
     if (!workspace || !aligned16(workspace) || workspace_bytes < decay_workspace_bytes(B, H, H_kv, grid_h * grid_w, d_k, d_v, dtype, true)) return DIG_ERR_WORKSPACE;
     DecayCall c{};
     c.q = q; c.k = k; c.v = v; c.strides = strides; c.log_decay = log_decay_per_head; c.lengths = lengths; c.d_out = d_out; c.s_in = s_in; c.ds_out = ds_out;

@@ -39,7 +39,7 @@ def test_decay_refusals(L):
             n=1 << 30):
         return L.dig_decay_fwd(q, k, v, strides, decay, lengths, s_in, out, s_out, B, H, Hk, gh, gw, dk, dv, dir, dtype, ws, n, None)
 
-    for bad in (dict(q=None), dict(k=OK + 8), dict(v=None), dict(decay=None), dict(out=None), dict(s_in=OK + 4), dict(s_out=OK + 4), dict(lengths=OK + 2), dict(H=3), dict(dir=4),
+    for bad in (dict(q=None), dict(k=OK + 8), dict(v=None), dict(decay=None), dict(out=None), dict(s_in=OK + 4), dict(s_out=OK + 4), dict(s_in=OK, s_out=OK), dict(lengths=OK + 2), dict(H=3), dict(dir=4),
                 dict(dir=-1), dict(dtype=2), dict(dk=4), dict(gw=0), dict(strides=(ctypes.c_longlong * 6)(4, 128, 128, 128, 128, 128)),
                 dict(strides=(ctypes.c_longlong * 6)(128, -128, 128, 128, 128, 128)), dict(decay=floats(-0.1, 0.2)), dict(decay=floats(float("nan"), -0.2)),
                 dict(decay=floats(-0.1, float("-inf")))):
@@ -52,7 +52,7 @@ def test_decay_refusals(L):
     def bwd(q=OK, d_out=OK, ds_out=None, dq=OK, dk=OK, dv=OK, ds_in=None, decay=lam, lengths=None, dir=0, n=1 << 30, dtype=1):
         return L.dig_decay_bwd(q, OK, OK, None, decay, lengths, d_out, None, ds_out, dq, dk, dv, ds_in, 1, 2, 2, 4, 4, 64, 64, dir, dtype, OK, n, None)
 
-    for bad in (dict(q=None), dict(d_out=None), dict(dq=None), dict(dk=None), dict(dv=OK + 8), dict(ds_out=OK + 8), dict(ds_in=OK + 8), dict(decay=floats(1.0, -1.0)), dict(dtype=2)):
+    for bad in (dict(q=None), dict(d_out=None), dict(dq=None), dict(dk=None), dict(dv=OK + 8), dict(ds_out=OK + 8), dict(ds_in=OK + 8), dict(ds_in=OK, ds_out=OK), dict(decay=floats(1.0, -1.0)), dict(dtype=2)):
         assert bwd(**bad) == dig.DIG_ERR_INVALID_ARG, bad
     assert bwd(n=0) == dig.DIG_ERR_WORKSPACE and bwd(lengths=OK, dir=3) == dig.DIG_ERR_UNSUPPORTED
 
