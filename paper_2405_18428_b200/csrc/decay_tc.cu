@@ -11,9 +11,9 @@
 //
 // One CTA per SM works through a list of segments; its warps have parts of their own, so that the loads of one tile, the scores of the
 // next, the state of this one and the results of the one before overlap:
-//   warps 0 .. 7    scores to decayed scores; results of the tile before to global memory
-//   warps 8 .. 15   decayed keys, state
-//   warps 16 .. 19  results
+//   warps 0 .. 7    scores to decayed scores; of heads beyond 64 channels decayed keys
+//   warps 8 .. 15   state; of heads up to 64 channels decayed keys
+//   warps 16 .. 19  results, through shared memory to global memory
 //   warps 20 .. 22  loads of q, k, v;  warp 23  products
 // Five parts on every scheduler share its instruction cache: loops are kept short and rolled, and what is rare stands apart.  Unrolled, two
 // thirds of the warps' time went by waiting for instructions (4 x 4096 tokens of 12 heads of 64 channels: 60 us).
@@ -62,21 +62,15 @@ __device__ __forceinline__ constexpr int p_col(int kk) { return (kk >> 2) * 16 +
 
 // Barriers: two of each, tile i of the CTA's list uses i & 1 in phase i >> 1.  Nobody may be two phases behind on one: each is completed
 // again only after all that wait for it have gone on.
-constexpr uint32_t kNone = 0xffffffffu;
+constexpr uint32_t kNone = 0xffffffffu;                          // a row that is not written
 struct Bars {
     uint64_t q[2], k[2], v[2];           // loaded
     uint64_t s[2], i[2], u[2], o[2];     // products done: scores; scores and what the state gives; the tile's state; outputs
     uint64_t p[2], kd[2], x[2];          // written: decayed scores, decayed keys, state
     uint64_t uf[2], of[2];               // read: the tile's state; outputs and what the state gives
-    uint64_t r[2], rf[2];                // results written to shared memory; read there
     uint32_t tmem;
     int dead;                            // a wait gave up: no more waiting
 };
-struct Ctl : Bars {
-    uint32_t at[T];                      // rows of the tile whose results are on their way: in 16 bytes from the output's start, or kNone
-    int pass, nch;                       // its pass, and chunks of a row (0: they have gone out already)
-};
-
 __host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, bool a_mn, bool b_mn) { return idesc_f16(M, N, a_mn, b_mn) | (1u << 7) | (1u << 10); }
 __device__ __forceinline__ uint64_t kmajor(uint32_t a, uint32_t ch) { return make_desc(a, ch, 128, 0); }
 __device__ __forceinline__ uint64_t mnmajor(uint32_t a, uint32_t ch) { return make_desc(a, 128, ch, 0); }
@@ -302,7 +296,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
 {
     using C = Cfg<D>;
     extern __shared__ char raw[];
-    __shared__ Ctl ctl;
+    __shared__ Bars ctl;
     char *sm = raw + (-smem_u32(raw) & 1023);
     const uint32_t base = smem_u32(sm);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -313,7 +307,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
             mbar_init(&ctl.q[j], 32); mbar_init(&ctl.k[j], 32); mbar_init(&ctl.v[j], 32);
             mbar_init(&ctl.s[j], 1); mbar_init(&ctl.i[j], 1); mbar_init(&ctl.u[j], 1); mbar_init(&ctl.o[j], 1);
             mbar_init(&ctl.p[j], kScore); mbar_init(&ctl.kd[j], kState); mbar_init(&ctl.x[j], kState);
-            mbar_init(&ctl.uf[j], kState); mbar_init(&ctl.of[j], kOut); mbar_init(&ctl.r[j], kOut); mbar_init(&ctl.rf[j], kScore);
+            mbar_init(&ctl.uf[j], kState); mbar_init(&ctl.of[j], kOut);
         }
         ctl.dead = 0;
         fence_barrier_init();
@@ -453,35 +447,6 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
     } else if (warp < kScore) {
         const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;
         const uint32_t mine = tm + ((uint32_t)(quarter * 32) << 16);
-        // Results of tile j from shared to global memory: consecutive lanes have the chunks of a row.  (A bulk copy a row, issued by four warps,
-        // took 5700 cycles a tile.)
-        auto rows_out = [&](int j) {
-            wait(&ctl, ctl.r, j, status);
-            constexpr int LANES = D == 128 ? 16 : 8, STEP = kScore * 32 / LANES;
-            const int nch = ctl.nch, c = tid % LANES;
-            char *out = (char *)a.pass[ctl.pass].out;
-            const char *from = sm + C::R + c * CH;
-            if (c < nch) {
-#pragma unroll 1
-                for (int r0 = tid / LANES; r0 < T; r0 += 4 * STEP) {
-                    uint32_t at[4];
-                    uint4 y[4];
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        at[m] = ctl.at[r0 + m * STEP];
-                        y[m] = *reinterpret_cast<const uint4 *>(from + (r0 + m * STEP) * 16);
-                    }
-#pragma unroll
-                    for (int m = 0; m < 4; ++m)
-                        if (at[m] != kNone) *reinterpret_cast<uint4 *>(out + (size_t)(at[m] + c) * 16) = y[m];
-                }
-            }
-            if constexpr (C::REST > 0) {         // chunks 8 and 9, a row a thread
-                const int ch = LANES + tid / T, r0 = tid % T;
-                if (ch < nch && ctl.at[r0] != kNone) *reinterpret_cast<uint4 *>(out + (size_t)(ctl.at[r0] + ch) * 16) = *reinterpret_cast<const uint4 *>(sm + C::R + ch * CH + r0 * 16);
-            }
-            warp_arrive(&ctl.rf[j & 1]);
-        };
         auto keys = [&](const Item &w, int t, int j) {       // of the item's tile t, the list's tile j
             wait(&ctl, ctl.k, j, status);
             if (t + 1 < w.t_end) {
@@ -539,11 +504,9 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
                 tc_fence_before_sync();
                 warp_arrive(&ctl.p[i & 1]);
                 if (C::IN_PLACE) keys(w, t, i);  // the scores have them
-                if (i > 0) rows_out(i - 1);
                 if (C::KEYS_BY_SCORE && !C::IN_PLACE && t + 1 < w.t_end) keys(w, t + 1, i + 1);
             }
         }
-        if (i > 0) rows_out(i - 1);
     } else if (warp < kScore + kState) {
         const int quarter = warp & 3, half = (warp >> 2) & 1, row = quarter * 32 + lane, me = tid - kScore * 32;
         const uint32_t mine = tm + ((uint32_t)(quarter * 32) << 16);
@@ -651,6 +614,7 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
             const Pass &ps = a.pass[w.pass];
             const float lam = a.lam.v[w.h];
             const int dv = ps.dv, nch = dv / 8;
+            const uint32_t nch_inv = 65536 / nch + 1;        // e / nch for e < 512: off by less than 512 / 65536, less than 1 / nch
             const bool start = w.seg > 0 || ps.x0;
             const size_t tok_out = (size_t)a.H * dv, head_out = (size_t)w.b * a.L * tok_out + (size_t)w.h * dv;
             for (int t = w.t0; t < w.t_end; ++t, ++i) {
@@ -660,14 +624,9 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
                 const float2 w2 = make_float2(wr, wr);
                 const int mt = token_or_not(a, ps.dir, p0 + row, w.n), token = mt >= 0 ? mt : ~mt;
                 const size_t at = head_out + (size_t)token * tok_out;
-                if (i > 0) wait(&ctl, ctl.rf, i - 1, status);        // the results before have been read
+                const uint32_t here = token < a.L ? (uint32_t)(at / 8) : kNone;
                 wait(&ctl, ctl.o, i, status);
                 tc_fence_after_sync();
-                ctl.at[row] = token < a.L ? (uint32_t)(at / 8) : kNone;
-                if (tid == (kScore + kState) * 32) {
-                    ctl.pass = w.pass;
-                    ctl.nch = ps.out_f32 ? 0 : nch;
-                }
 #pragma unroll 1
                 for (int c = 0; c < D; c += 16) {
                     uint32_t r[16], y[16];
@@ -701,7 +660,29 @@ __global__ void __launch_bounds__(kThreads, 1) decay_pass(const __grid_constant_
                         *reinterpret_cast<uint4 *>(R + (c + e) / 8 * CH + row * 16) = make_uint4(pack(f(r[e]), f(r[e + 1])), pack(f(r[e + 2]), f(r[e + 3])), pack(f(r[e + 4]), f(r[e + 5])),
                                                                                                 pack(f(r[e + 6]), f(r[e + 7])));
                 }
-                warp_arrive(&ctl.r[i & 1]);
+                // The warp's 32 rows from shared to global memory, consecutive lanes the chunks of a row.  (A bulk copy a row took 5700 cycles a
+                // tile; by the scores' warps, a tile later, 2% longer.)
+                __syncwarp();
+                if (!ps.out_f32) {
+#pragma unroll 1
+                    for (int e0 = lane; e0 < 32 * nch; e0 += 64) {
+                        uint32_t to[2];
+                        uint4 y[2];
+                        int c[2];
+#pragma unroll
+                        for (int m = 0; m < 2; ++m) {
+                            const int e = min(e0 + m * 32, 32 * nch - 1), r = (int)(e * nch_inv >> 16);
+                            c[m] = e - r * nch;
+                            to[m] = __shfl_sync(0xffffffffu, here, r);
+                            if (e0 + m * 32 != e) to[m] = kNone;
+                            y[m] = *reinterpret_cast<const uint4 *>(R + c[m] * CH + (quarter * 32 + r) * 16);
+                        }
+#pragma unroll
+                        for (int m = 0; m < 2; ++m)
+                            if (to[m] != kNone) *reinterpret_cast<uint4 *>((char *)ps.out + (size_t)(to[m] + c[m]) * 16) = y[m];
+                    }
+                }
+                __syncwarp();
             }
             // whole tiles behind the end
             for (int p = max(w.t_end, w.t0) * T + (warp - kScore - kState); p < min(w.t1 * T, a.L); p += kOut)
