@@ -281,6 +281,7 @@ dig_status dig_gla_bwd_multi(const void *q, const void *k, const void *v, const 
  *   out behind the end of a sequence are zeros, what q, k and v hold there is not used.  Row orders only (else DIG_ERR_UNSUPPORTED).
  *   s_in: state before the first token, fp32 [B][H][d_k][d_v], NULL = 0; s_out: receives the state after the last token, or NULL; not
  *   the same array (DIG_ERR_INVALID_ARG).
+ * Results overlap no input (here and in dig_decay_bwd).
  * fp32 storage: fp32 FMA arithmetic.  bf16 storage: q, k and v enter the products as they are, decayed scores, states and (for out) decayed
  * keys as bf16, sums in fp32; s_out is summed apart with decayed keys of 24 bits and has fp32 accuracy.
  * A NaN or an infinity in v reaches rows of the same 32 positions before it (products with zeros), never earlier ones. */
@@ -307,7 +308,8 @@ dig_status dig_decay_step(const void *q, const void *k, const void *v, const flo
 /* Rotary positions with several axes (height and width of a token grid, time of a video): pair i of every head's channels is turned by
  * the angle positions[b][l][axes[i]] * freqs[i], by its negative with `inverse` (which is the gradient).
  *   pair i: channels (2 i, 2 i + 1) where `interleaved`, else (i, i + n_pairs); channels from 2 n_pairs on stay as they are.
- *   q: [B][L][H][d]; k: [B][L][H_k][d] or NULL; q_out, k_out: the same, dense, or the inputs themselves (in place).
+ *   q: [B][L][H][d]; k: [B][L][H_k][d] or NULL; q_out, k_out: the same, dense, or the inputs themselves (in place).  Otherwise results overlap no
+ *   input, and q and k turned in place do not overlap.
  *   strides: HOST array of the batch and token strides of q and k in elements, multiples of 16 bytes, or NULL: dense.
  *   positions: int32 [pos_batches][L][n_axes], DEVICE, pos_batches 1 or B; any values.
  *   freqs: HOST array of n_pairs values (radians per position); axes: HOST array of n_pairs values in 0 .. n_axes - 1.

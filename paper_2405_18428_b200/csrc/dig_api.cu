@@ -588,6 +588,7 @@ dig_status dig_rope(const void *q, const void *k, const long long *strides, cons
     if (!strides_ok(strides, k ? 4 : 2, dtype)) return DIG_ERR_INVALID_ARG;
     for (int i = 0; i < n_pairs; ++i)
         if (axes[i] < 0 || axes[i] >= n_axes || !(freqs[i] >= -1e30 && freqs[i] <= 1e30)) return DIG_ERR_INVALID_ARG;
+    if (k && (q_out == k_out || q_out == k || k_out == q)) return DIG_ERR_INVALID_ARG;            // turned twice, or read after it is written
     return launch_rope(q, k, strides, positions, pos_batches, n_axes, freqs, axes, n_pairs, q_out, k_out, B, L, H, H_k, d, interleaved != 0, inverse != 0, dtype,
                        (cudaStream_t)cuda_stream);
 }

@@ -369,7 +369,8 @@ def dig_rope(q, k, positions, freqs, axes, *, interleaved=False, inverse=False, 
     """Turns pair i of every head's channels by positions[..., axes[i]] * freqs[i]; returns (q_out, k_out), k may be None.
 
     q: [B, L, H, d]; k: [B, L, H_k, d], the last two dimensions dense; positions: int32 [L, axes] or [B, L, axes].  Pairs are channels
-    (i, i + n), or (2i, 2i + 1) with `interleaved`; `inverse` turns back (the gradient); `inplace` writes to q and k."""
+    (i, i + n), or (2i, 2i + 1) with `interleaved`; `inverse` turns back (the gradient); `inplace` writes to q and k, which
+    must not overlap then."""
     return _binding().rope(q, k, positions, freqs, axes, interleaved, inverse, inplace)
 
 

@@ -67,14 +67,14 @@ def test_decay_refusals(L):
 def test_rope_refusals(L):
     from paper_2405_18428_b200 import dig
 
-    def rope(q=OK, k=OK, strides=None, pos=OK, pb=1, axes_n=2, freqs=(ctypes.c_double * 4)(1, 1, 1, 1), axes=(ctypes.c_int * 4)(0, 0, 1, 1), n=4, qo=OK, ko=OK, B=2, Lq=4, H=2, Hk=2,
+    def rope(q=OK, k=OK + 64, strides=None, pos=OK, pb=1, axes_n=2, freqs=(ctypes.c_double * 4)(1, 1, 1, 1), axes=(ctypes.c_int * 4)(0, 0, 1, 1), n=4, qo=OK, ko=OK + 64, B=2, Lq=4, H=2, Hk=2,
              d=8, dtype=1):
         return L.dig_rope(q, k, strides, pos, pb, axes_n, freqs, axes, n, qo, ko, B, Lq, H, Hk, d, 0, 0, dtype, None)
 
     nan = (ctypes.c_double * 4)(1, float("nan"), 1, 1)
     for bad in (dict(q=None), dict(pos=None), dict(pos=OK + 2), dict(freqs=None), dict(axes=None), dict(qo=None), dict(ko=None), dict(k=None), dict(q=OK + 8), dict(B=0), dict(Lq=0),
                 dict(H=0), dict(Hk=0), dict(d=12), dict(d=136), dict(dtype=2), dict(pb=3), dict(axes_n=0), dict(axes_n=1), dict(n=0), dict(n=5), dict(n=3), dict(freqs=nan),
-                dict(axes=(ctypes.c_int * 4)(0, -1, 1, 1)), dict(strides=(ctypes.c_longlong * 4)(8, 4, 8, 8))):
+                dict(axes=(ctypes.c_int * 4)(0, -1, 1, 1)), dict(ko=OK), dict(qo=OK + 64, ko=OK + 128), dict(qo=OK + 128, ko=OK), dict(strides=(ctypes.c_longlong * 4)(8, 4, 8, 8))):
         assert rope(**bad) == dig.DIG_ERR_INVALID_ARG, bad
     assert rope(B=1 << 20, pb=1, Lq=1 << 20) == rope(H=4097) == rope(H=70000) == dig.DIG_ERR_UNSUPPORTED
 

@@ -215,3 +215,79 @@ def test_gradient_against_differences():
         want = float((g.double() * step.double()).sum())
         # each loss is a sum of about 4000 values of size 10 known to about 1e-6
         assert abs(slope - want) <= 4e3 * 10 * 1e-6 + 1e-6 * abs(want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_further_apart_than_32_bits_count(dtype):
+    from paper_2405_18428_b200 import dig
+    L, H, d, apart = 1100, 2, 64, 1 << 22                    # the last row starts at 4.6e9 elements
+    storage = torch.bfloat16 if dtype == "bf16" else torch.float32
+    far = torch.empty(1, L, apart, dtype=storage, device="cuda")
+    near = torch.randn(1, L, 2 * H * d, device="cuda").to(storage)
+    far[:, :, :2 * H * d] = near
+    cut = lambda t: [x.unflatten(2, (-1, d)) for x in (t[:, :, :H * d], t[:, :, H * d:(H + 1) * d], t[:, :, (H + 1) * d:2 * H * d])]
+    d_out = torch.randn(1, L, H, d, device="cuda").to(storage)
+    lam = [-0.01, -0.5]
+    for direction in (1, 2):
+        runs = []
+        for t in (far, near):
+            q, k, v = cut(t)
+            runs.append((*dig.dig_decay_fwd(q, k, v, lam, 20, 55, direction, want_s_out=True), *dig.dig_decay_bwd(q, k, v, lam, d_out, 20, 55, direction, want_ds_in=True)))
+        assert all(torch.equal(a, b) for a, b in zip(*runs))
+    freqs, axes = dig.dig_rope_freqs((32,))
+    pos = torch.arange(L, device="cuda", dtype=torch.int32).view(L, 1)
+    want = dig.dig_rope(*cut(near)[:2], pos, freqs, axes)
+    assert all(torch.equal(a, b) for a, b in zip(dig.dig_rope(*cut(far)[:2], pos, freqs, axes), want))
+    turned = dig.dig_rope(*cut(far)[:2], pos, freqs, axes, inplace=True)
+    assert all(torch.equal(a, b) for a, b in zip(turned, want))
+    del far, turned, q, k, v, t
+    torch.cuda.empty_cache()
+
+
+def test_a_turn_in_place_needs_tensors_of_its_own():
+    from paper_2405_18428_b200 import dig
+    x = torch.randn(1, 16, 2, 64, device="cuda")
+    pos = torch.zeros(16, 1, dtype=torch.int32, device="cuda")
+    with pytest.raises(dig.DigError):
+        dig.dig_rope(x, x, pos, *dig.dig_rope_freqs((32,)), inplace=True)
+    a, b = dig.dig_rope(x, x, pos, *dig.dig_rope_freqs((32,)))
+    assert torch.equal(a, x) and torch.equal(b, x)
+
+
+@pytest.mark.parametrize("B,H,Hk,L,d", [(1, 6, 6, 256, 64), (5, 16, 4, 2500, 128), (128, 6, 6, 256, 64)])
+def test_the_final_state_is_there_for_what_follows(B, H, Hk, L, d):
+    """Uncut sequences: their final state is summed beside the passes.  On two streams at once, and as a replayed graph."""
+    from paper_2405_18428_b200 import dig
+    mk = lambda *s: torch.randn(*s, device="cuda").to(torch.bfloat16)
+    q, k, v, d_out = mk(B, L, H, d), mk(B, L, Hk, d), mk(B, L, Hk, d), mk(B, L, H, d)
+    s_in, ds_out = torch.randn(B, H, d, d, device="cuda"), torch.randn(B, H, d, d, device="cuda")
+    lam = [-0.002 * (h + 1) for h in range(H)]
+    token = q[:, 0].contiguous(), k[:, 0].contiguous(), v[:, 0].contiguous()
+
+    def run():
+        out, s = dig.dig_decay_fwd(q, k, v, lam, 1, L, s_in=s_in, want_s_out=True)
+        kept = s.clone()
+        step = dig.dig_decay_step(*token, lam, s)
+        grads = dig.dig_decay_bwd(q, k, v, lam, d_out, 1, L, s_in=s_in, ds_out=ds_out, want_ds_in=True)
+        return out.clone(), kept, s, step, *(g.clone() for g in grads)
+
+    want = run()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for _ in range(8):
+        for stream in streams:
+            with torch.cuda.stream(stream):
+                got.append(run())
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for g in got for a, b in zip(g, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        kept = run()
+    for t in kept:
+        t.zero_()
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(kept, want))
+    assert dig.dig_last_device_status() == dig.DIG_OK
