@@ -117,7 +117,7 @@ struct StepArgs {
 };
 // A CTA has one head of one sequence.  S = g S + k^T v, o = q S: a thread has four value channels of every `groups`-th state row.  Bound by
 // the state's bytes, in and out.  The rows of a batch are asked for together before the first is written: the state may be updated in
-// place, so no load would pass a store (192 sequences of 16 heads of 72 x 72: 31 us so).
+// place, so no load would pass a store (192 sequences of 16 heads of 72 x 72: 27 us, 4.7 TB/s).
 constexpr int kBatch = 8;
 template <typename S>
 __global__ void __launch_bounds__(256) decay_step(const __grid_constant__ StepArgs a)

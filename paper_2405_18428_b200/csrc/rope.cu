@@ -9,7 +9,7 @@
 namespace dig {
 namespace {
 
-constexpr int kMaxPairs = 64, kNT = 256, kMaxTokens = 8;
+constexpr int kMaxPairs = 64, kNT = 256, kMaxTokens = 8, kCtas = 4;          // kCtas: on an SM
 
 // Division of i < 2^31 through the reciprocal rounded up: the estimate is at most one too large.
 struct Div {
@@ -76,15 +76,27 @@ __device__ __forceinline__ void stv(T *p, const float (&f)[V])
     *reinterpret_cast<U *>(p) = u;
 }
 
+template <int V>
+__device__ __forceinline__ void angles(const float *p, float (&f)[V])
+{
+    if constexpr (V % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < V; i += 4) *reinterpret_cast<float4 *>(f + i) = load4(p + i);
+    } else if constexpr (V == 2) *reinterpret_cast<float2 *>(f) = *reinterpret_cast<const float2 *>(p);
+    else f[0] = p[0];
+}
+
 // V pairs per thread and turn: neighbours (2 i, 2 i + 1) where INTER, else (i, i + n).  kTurns turns' loads are on their way together, the first
-// ones while the angles are formed (with the angles first: 48 us for 16384 tokens of 32 heads of 72).
+// ones while the angles are formed (with the angles first: 48 us for 16384 tokens of 32 heads of 72; 34 so, 4.4 TB/s, where a plain copy of as
+// many bytes takes 27).
 constexpr int kTurns = 4;
 template <typename T, int V, bool INTER>
-__global__ void __launch_bounds__(kNT, 4) rope(const __grid_constant__ RopeArgs a)
+__global__ void __launch_bounds__(kNT, kCtas) rope(const __grid_constant__ RopeArgs a)
 {
     constexpr int E = INTER ? 2 * V : V, HALVES = INTER ? 1 : 2;
     using U = typename Vec<T, E>::U;
-    __shared__ float2 cs[kMaxTokens * kMaxPairs];            // cosine, sine
+    // apart, so that lanes read consecutive vectors of them
+    __shared__ __align__(16) float cosines[kMaxTokens * kMaxPairs], sines[kMaxTokens * kMaxPairs];
     __shared__ double turns[kMaxPairs];
     __shared__ int axis[kMaxPairs];
     __shared__ long long xo[2][kMaxTokens], yo[2][kMaxTokens];               // where a token's q and k stand
@@ -134,9 +146,7 @@ __global__ void __launch_bounds__(kNT, 4) rope(const __grid_constant__ RopeArgs 
         const int t = i / n, j = i - t * n;
         const uint32_t tok = (uint32_t)(first + t), b = tok / (uint32_t)a.L;
         const double z = a.pos[b * a.pos_batch + (long long)(tok - b * a.L) * a.axes + axis[j]] * turns[j];
-        float2 v;
-        sincospif((float)(2.0 * (z - rint(z))), &v.y, &v.x);
-        cs[i] = v;
+        sincospif((float)(2.0 * (z - rint(z))), sines + i, cosines + i);
     }
     __syncthreads();
     for (uint32_t i0 = threadIdx.x; i0 < count; i0 += kTurns * kNT) {
@@ -147,15 +157,17 @@ __global__ void __launch_bounds__(kNT, 4) rope(const __grid_constant__ RopeArgs 
             if (i >= count) break;
             const int which = to[m] & 1;
             T *y = (T *)a.y[which] + yo[which][to[m] >> 1 & 7] + (to[m] >> 4);
-            const float2 *w = cs + pair[m];
             float f[E];
+            __align__(16) float co[V], si[V];
+            angles<V>(cosines + pair[m], co);
+            angles<V>(sines + pair[m], si);
             unpack<T, E>(raw[m][0], f);
             if constexpr (INTER) {
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
                     const float p = f[2 * e], q = f[2 * e + 1];
-                    f[2 * e] = p * w[e].x - q * w[e].y;
-                    f[2 * e + 1] = p * w[e].y + q * w[e].x;
+                    f[2 * e] = p * co[e] - q * si[e];
+                    f[2 * e + 1] = p * si[e] + q * co[e];
                 }
                 stv<T, E>(y, f);
             } else {
@@ -164,8 +176,8 @@ __global__ void __launch_bounds__(kNT, 4) rope(const __grid_constant__ RopeArgs 
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
                     const float p = f[e], q = g[e];
-                    f[e] = p * w[e].x - q * w[e].y;
-                    g[e] = p * w[e].y + q * w[e].x;
+                    f[e] = p * co[e] - q * si[e];
+                    g[e] = p * si[e] + q * co[e];
                 }
                 stv<T, E>(y, f);
                 stv<T, E>(y + n, g);
@@ -212,8 +224,6 @@ dig_status launch_rope(const void *q, const void *k, const long long *strides, c
     }
     a.pos = positions; a.pos_batch = pos_batches > 1 ? (long long)L * n_axes : 0;
     a.L = L; a.d = d; a.n = n_pairs; a.axes = n_axes; a.total = (long long)B * L;
-    a.tokens = (int)(a.total / (148 * 8));
-    a.tokens = a.tokens < 1 ? 1 : a.tokens > kMaxTokens ? kMaxTokens : a.tokens;
     if (a.total > 0x7fffffffll) return DIG_ERR_UNSUPPORTED;
     for (int i = 0; i < n_pairs; ++i) {
         a.turns[i] = (inverse ? -freqs[i] : freqs[i]) * 0.15915494309189533577;
@@ -222,6 +232,16 @@ dig_status launch_rope(const void *q, const void *k, const long long *strides, c
     const bool f = dtype == DIG_F32;
     const int v = interleaved ? (f ? (n_pairs % 2 == 0 ? 2 : 1) : n_pairs % 4 == 0 ? 4 : 1) : f ? (n_pairs % 4 == 0 ? 4 : 1) : n_pairs % 8 == 0 ? 8 : n_pairs % 4 == 0 ? 4 : 1;
     const uint32_t units = n_pairs / v, per = units * (heads[0] + heads[1]);
+    // The number of tokens with which the rounds of CTAs take the fewest turns, the largest of those, or the smallest where one round holds
+    // all (16384 tokens of 32 heads of 72 channels, 7 tokens a CTA: 34 us; 8, the most that there are angles for, 36).
+    long long least = 0;
+    for (int t = kMaxTokens; t >= 1; --t) {
+        const long long ctas = (a.total + t - 1) / t, rounds = (ctas + 148 * kCtas - 1) / (148 * kCtas), turns = rounds * ((t * per + kNT - 1) / kNT);
+        if (least == 0 || turns < least || (turns == least && rounds == 1)) {
+            least = turns;
+            a.tokens = t;
+        }
+    }
     a.by_head = {units, 0xffffffffu / units + 1};
     a.by_token = {per, 0xffffffffu / per + 1};
     using bf16 = __nv_bfloat16;
