@@ -19,6 +19,7 @@
 #include <vector>
 
 #include "dig_gla.h"
+#include "row_sets.h"
 
 namespace {
 
@@ -697,11 +698,9 @@ PyObject *rope(PyObject *const *a)
     const int inter = truth(a[5]), inv = truth(a[6]);
     void *qop = qo.data_ptr(), *kop = kp ? ko.data_ptr() : nullptr, *s = on.stream();
     if (in_place)           // rows that coincide cannot all be written
-        for (int i = 0; i < (kp ? 2 : 1); ++i) {
-            const Tensor &t = i ? ko : qo;
-            if (!t.is_non_overlapping_and_dense() && ((B > 1 && t.stride(0) < (L - 1) * strides[2 * i + 1] + t.size(2) * d && t.stride(1) < (B - 1) * strides[2 * i] + t.size(2) * d) || (L > 1 && t.stride(1) < t.size(2) * d)))
+        for (int i = 0; i < (kp ? 2 : 1); ++i)
+            if (!dig::distinct({(int)B, (int)L, strides[2 * i], strides[2 * i + 1], (i ? Hk : q.size(2)) * d}))
                 raise(PyExc_ValueError, std::string(i ? "k" : "q") + ": rows overlap, they cannot be turned in place");
-        }
     CALL(dig_rope(qp, kp, strides, pp, batched ? (int)B : 1, (int)pos.size(-1), freqs.data(), axes.data(), (int)freqs.size(), qop, kop, (int)B, (int)L, (int)q.size(2), Hk,
                   (int)d, inter, inv, dtype, s), "dig_rope");
     return pack({qo, ko});

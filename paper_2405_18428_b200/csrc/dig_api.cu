@@ -8,6 +8,7 @@
 
 #include "decay_plan.cuh"
 #include "dig_common.cuh"
+#include "row_sets.h"
 #include "sweep.cuh"
 #include "umma.cuh"
 
@@ -589,6 +590,13 @@ dig_status dig_rope(const void *q, const void *k, const long long *strides, cons
     for (int i = 0; i < n_pairs; ++i)
         if (axes[i] < 0 || axes[i] >= n_axes || !(freqs[i] >= -1e30 && freqs[i] <= 1e30)) return DIG_ERR_INVALID_ARG;
     if (k && (q_out == k_out || q_out == k || k_out == q)) return DIG_ERR_INVALID_ARG;            // turned twice, or read after it is written
+    // in place every row is an output: none is turned twice, nor by two CTAs at once
+    const long long dense_q = (long long)H * d, dense_k = (long long)H_k * d;
+    const RowSet rq{B, L, strides ? strides[0] : dense_q * L, strides ? strides[1] : dense_q, dense_q};
+    const RowSet rk{B, L, k && strides ? strides[2] : dense_k * L, k && strides ? strides[3] : dense_k, dense_k};
+    if ((q_out == q && !distinct(rq)) || (k && k_out == k && !distinct(rk))) return DIG_ERR_INVALID_ARG;
+    if (k && (q_out == q || k_out == k) && !apart(rq, rk, ((long long)reinterpret_cast<uintptr_t>(k) - (long long)reinterpret_cast<uintptr_t>(q)) / (dtype == DIG_F32 ? 4 : 2)))
+        return DIG_ERR_INVALID_ARG;
     return launch_rope(q, k, strides, positions, pos_batches, n_axes, freqs, axes, n_pairs, q_out, k_out, B, L, H, H_k, d, interleaved != 0, inverse != 0, dtype,
                        (cudaStream_t)cuda_stream);
 }

@@ -370,7 +370,7 @@ def dig_rope(q, k, positions, freqs, axes, *, interleaved=False, inverse=False, 
 
     q: [B, L, H, d]; k: [B, L, H_k, d], the last two dimensions dense; positions: int32 [L, axes] or [B, L, axes].  Pairs are channels
     (i, i + n), or (2i, 2i + 1) with `interleaved`; `inverse` turns back (the gradient); `inplace` writes to q and k, which
-    must not overlap then."""
+    must not overlap then, one another nor themselves (a batch broadcast from one sequence)."""
     return _binding().rope(q, k, positions, freqs, axes, interleaved, inverse, inplace)
 
 
