@@ -311,7 +311,7 @@ dig_status dig_decay_step(const void *q, const void *k, const void *v, const flo
  *   q: [B][L][H][d]; k: [B][L][H_k][d] or NULL; q_out, k_out: the same, dense, or the inputs themselves (in place).  Otherwise results overlap no
  *   input.  Rows turned in place are distinct, those of q and k from one another too (else DIG_ERR_INVALID_ARG; so are q and k in place with
  *   both strides different and memory that interleaves).
- *   strides: HOST array of the batch and token strides of q and k in elements, multiples of 16 bytes, or NULL: dense.
+ *   strides: HOST array of the batch and token strides of q and (where there are keys) k in elements, multiples of 16 bytes, or NULL: dense.
  *   positions: int32 [pos_batches][L][n_axes], DEVICE, pos_batches 1 or B; any values.
  *   freqs: HOST array of n_pairs values (radians per position); axes: HOST array of n_pairs values in 0 .. n_axes - 1.
  *   H, H_k: at most 4096; d: a multiple of 8, 8..128; d - 2 n_pairs a multiple of 4.  `dtype`: DIG_F32 or DIG_BF16.

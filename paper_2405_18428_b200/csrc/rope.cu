@@ -215,7 +215,7 @@ dig_status launch_rope(const void *q, const void *k, const long long *strides, c
     const int heads[2] = {H, k ? H_k : 0};
     const void *x[2] = {q, k};
     void *y[2] = {q_out, k_out};
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < (k ? 2 : 1); ++i) {              // without keys the strides may end with those of q
         a.x[i] = x[i]; a.y[i] = y[i]; a.heads[i] = heads[i];
         a.yt[i] = (long long)heads[i] * d; a.yb[i] = a.yt[i] * L;
         a.xb[i] = strides ? strides[2 * i] : a.yb[i];
