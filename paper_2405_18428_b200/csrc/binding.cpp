@@ -86,6 +86,12 @@ std::string text(at::IntArrayRef s)
     for (size_t i = 0; i < s.size(); ++i) t += (i ? ", " : "") + std::to_string(s[i]);
     return t + (s.size() == 1 ? ",)" : ")");
 }
+// The library takes sizes of 31 bits; larger ones would be cut to them.
+int size31(int64_t n, const char *name)
+{
+    if (n > INT_MAX) raise(PyExc_ValueError, std::string(name) + ": a dimension of " + std::to_string(n) + " is too large");
+    return (int)n;
+}
 // Device pointer of a checked tensor.
 void *dev(const Tensor &t, ScalarType st, const char *name)
 {
@@ -401,10 +407,10 @@ PyObject *gla_fwd_outgate(PyObject *const *a)
 }
 
 // The rows of a tensor [..., d].
-void rows_of(const Tensor &o, int &d, long long &rows)
+void rows_of(const Tensor &o, int &d, long long &rows, const char *name)
 {
-    if (o.dim() < 1 || o.size(-1) < 1) raise(PyExc_ValueError, "o: need rows of at least one value, got shape " + text(o.sizes()));
-    d = (int)o.size(-1);
+    if (o.dim() < 1 || o.size(-1) < 1) raise(PyExc_ValueError, std::string(name) + ": need rows of at least one value, got shape " + text(o.sizes()));
+    d = size31(o.size(-1), name);
     rows = o.numel() / d;
 }
 // o r ln_w ln_b eps f32_out
@@ -413,7 +419,7 @@ PyObject *outgate_fwd(PyObject *const *a)
     const Tensor &o = tensor(a[0], "o");
     int d;
     long long rows;
-    rows_of(o, d, rows);
+    rows_of(o, d, rows, "o");
     const int dtype = dtype_of(o, truth(a[5]));
     const ScalarType st = storage(dtype);
     const void *op = dev(o, st, "o"), *rp = dev(a[1], st, o.sizes(), "r", o);
@@ -430,7 +436,7 @@ PyObject *outgate_bwd(PyObject *const *a)
     const Tensor &o = tensor(a[0], "o");
     int d;
     long long rows;
-    rows_of(o, d, rows);
+    rows_of(o, d, rows, "o");
     const int dtype = dtype_of(o, truth(a[7]));
     const ScalarType st = storage(dtype);
     const void *op = dev(o, st, "o"), *rp = dev(a[1], st, o.sizes(), "r", o), *zp = dev(a[2], st, o.sizes(), "dz", o);
@@ -529,6 +535,7 @@ void *rows(const Tensor &t, ScalarType st, const char *name, const Tensor &like,
     if (t.device() != like.device()) raise(PyExc_ValueError, std::string(name) + ": on " + t.device().str() + ", the other tensors on " + like.device().str());
     const int64_t H = t.size(2), d = t.size(3);
     if (t.numel() == 0) raise(PyExc_ValueError, std::string(name) + ": empty, shape " + text(t.sizes()));
+    for (const int64_t n : t.sizes()) size31(n, name);
     if ((d > 1 && t.stride(3) != 1) || (H > 1 && t.stride(2) != d))
         raise(PyExc_ValueError, std::string(name) + ": the last two dimensions have to be dense, got strides " + text(t.strides()));
     strides[1] = t.size(1) > 1 ? t.stride(1) : H * d;
@@ -637,6 +644,7 @@ PyObject *decay_step(PyObject *const *a)
     if (k.dim() != 3 || k.size(1) < 1 || q.size(1) % k.size(1) != 0) raise(PyExc_ValueError, "k: shape " + text(k.sizes()) + " does not go with q of " + text(q.sizes()));
     if (v.dim() != 3) raise(PyExc_ValueError, "v: need 3 dimensions [B, H_kv, d_v], got shape " + text(v.sizes()));
     const int64_t B = q.size(0), H = q.size(1), Hk = k.size(1), dk = q.size(2), dv = v.size(2);
+    for (const int64_t n : {B, H, Hk, dk, dv}) size31(n, "q, k, v");
     const int dtype = dtype_of(q, false);
     const ScalarType st = storage(dtype);
     const void *qp = dev(q, st, "q"), *kp = dev(k, st, {B, Hk, dk}, "k", q), *vp = dev(v, st, {B, Hk, dv}, "v", q);
@@ -670,6 +678,7 @@ PyObject *rope(PyObject *const *a)
     const bool batched = pos.dim() == 3;
     if (!(pos.dim() == 2 || (batched && pos.size(0) == B)) || pos.size(-2) != L) raise(PyExc_ValueError, "positions: need [L, axes] or [B, L, axes], got shape " + text(pos.sizes()));
     const int *pp = (const int *)dev(pos, ScalarType::Int, pos.sizes(), "positions", q);
+    const int n_axes = size31(pos.size(-1), "positions");
     std::vector<double> freqs;
     std::vector<int> axes;
     for (int which = 0; which < 2; ++which) {
@@ -701,7 +710,7 @@ PyObject *rope(PyObject *const *a)
         for (int i = 0; i < (kp ? 2 : 1); ++i)
             if (!dig::distinct({(int)B, (int)L, strides[2 * i], strides[2 * i + 1], (i ? Hk : q.size(2)) * d}))
                 raise(PyExc_ValueError, std::string(i ? "k" : "q") + ": rows overlap, they cannot be turned in place");
-    CALL(dig_rope(qp, kp, strides, pp, batched ? (int)B : 1, (int)pos.size(-1), freqs.data(), axes.data(), (int)freqs.size(), qop, kop, (int)B, (int)L, (int)q.size(2), Hk,
+    CALL(dig_rope(qp, kp, strides, pp, batched ? (int)B : 1, n_axes, freqs.data(), axes.data(), (int)freqs.size(), qop, kop, (int)B, (int)L, (int)q.size(2), Hk,
                   (int)d, inter, inv, dtype, s), "dig_rope");
     return pack({qo, ko});
 }
@@ -711,7 +720,7 @@ int groups_of(const Tensor &t, int D, const char *name)
 {
     if ((t.dim() != 1 && t.dim() != 2) || t.size(-1) != D || t.numel() == 0)
         raise(PyExc_ValueError, std::string(name) + ": need [" + std::to_string(D) + "] or [groups, " + std::to_string(D) + "], got shape " + text(t.sizes()));
-    return t.dim() == 1 ? 1 : (int)t.size(0);
+    return t.dim() == 1 ? 1 : size31(t.size(0), name);
 }
 // x w b eps
 PyObject *layernorm_fwd(PyObject *const *a)
@@ -720,7 +729,7 @@ PyObject *layernorm_fwd(PyObject *const *a)
     int D, groups = 1;
     long long rows;
     if (x.dim() < 1 || x.numel() == 0) raise(PyExc_ValueError, "x: need rows of at least one value, got shape " + text(x.sizes()));
-    rows_of(x, D, rows);
+    rows_of(x, D, rows, "x");
     const int dtype = dtype_of(x, false);
     const ScalarType st = storage(dtype);
     const void *xp = dev(x, st, "x");
@@ -752,7 +761,7 @@ PyObject *layernorm_bwd(PyObject *const *a)
     int D, groups = 1;
     long long rows;
     if (x.dim() < 1 || x.numel() == 0) raise(PyExc_ValueError, "x: need rows of at least one value, got shape " + text(x.sizes()));
-    rows_of(x, D, rows);
+    rows_of(x, D, rows, "x");
     const int dtype = dtype_of(x, false);
     const ScalarType st = storage(dtype);
     const void *xp = dev(x, st, "x"), *gp = dev(a[1], st, x.sizes(), "dy", x);
