@@ -281,7 +281,7 @@ dig_status dig_gla_bwd_multi(const void *q, const void *k, const void *v, const 
  *   out behind the end of a sequence are zeros, what q, k and v hold there is not used.  Row orders only (else DIG_ERR_UNSUPPORTED).
  *   s_in: state before the first token, fp32 [B][H][d_k][d_v], NULL = 0; s_out: receives the state after the last token, or NULL; not
  *   the same array (DIG_ERR_INVALID_ARG).
- * Results overlap no input (here and in dig_decay_bwd).
+ * Results overlap no input and no other result (here, in dig_decay_bwd and in dig_decay_step, but for its state in place).
  * fp32 storage: fp32 FMA arithmetic.  bf16 storage: q, k and v enter the products as they are, decayed scores, states and (for out) decayed
  * keys as bf16, sums in fp32; s_out is summed apart with decayed keys of 24 bits and has fp32 accuracy.
  * A NaN or an infinity in v reaches rows of the same 32 positions before it (products with zeros), never earlier ones. */

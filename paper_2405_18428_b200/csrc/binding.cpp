@@ -546,6 +546,51 @@ void *rows(const Tensor &t, ScalarType st, const char *name, const Tensor &like,
     return t.data_ptr();
 }
 
+// Dense tensors that a result must not overlap.
+void apart(std::initializer_list<const Tensor *> reads, const Tensor &t, const char *name)
+{
+    const char *p = (const char *)t.data_ptr(), *end = p + t.numel() * t.element_size();
+    for (const Tensor *r : reads) {
+        const char *o = (const char *)r->data_ptr();
+        if (p < o + r->numel() * r->element_size() && o < end) raise(PyExc_ValueError, std::string(name) + ": overlaps another tensor of the call");
+    }
+}
+// What a result must not overlap: rows of the inputs, and dense tensors.
+struct Reads {
+    struct One {
+        const char *name, *p;
+        dig::RowSet rows;                // in bytes
+    };
+    std::vector<One> all;
+    void add(const Tensor &t, const char *name, const long long *strides)
+    {
+        const long long e = t.element_size();
+        all.push_back({name, (const char *)t.data_ptr(), {(int)t.size(0), (int)t.size(1), strides[0] * e, strides[1] * e, t.size(2) * t.size(3) * e}});
+    }
+    void add(const Tensor &t, const char *name)
+    {
+        all.push_back({name, (const char *)t.data_ptr(), {1, 1, 0, 0, (long long)t.numel() * (long long)t.element_size()}});
+    }
+    void add(PyObject *o, const char *name)
+    {
+        if (!none(o)) add(tensor(o, name), name);
+    }
+    // A result, or scratch, that the caller gave; the ones after it must not overlap it either.
+    void write(const Tensor &t, const char *name)
+    {
+        const long long n = (long long)t.numel() * (long long)t.element_size();
+        const char *p = (const char *)t.data_ptr();
+        for (const One &r : all)
+            if (dig::rows_meet_block(r.rows, (long long)(uintptr_t)p - (long long)(uintptr_t)r.p, n))
+                raise(PyExc_ValueError, std::string(name) + ": overlaps " + r.name);
+        add(t, name);
+    }
+    void write(PyObject *o, const char *name)
+    {
+        if (!none(o)) write(tensor(o, name), name);
+    }
+};
+
 struct Decay {
     const Tensor &q_t;
     int B, L, H, Hk, dk, dv, gh, gw, dtype;
@@ -571,6 +616,14 @@ struct Decay {
         B = (int)n[0]; L = (int)n[1]; H = (int)n[2]; Hk = (int)k_t.size(2); dk = (int)n[3]; dv = (int)v_t.size(3);
         decay = numbers(a[3], H, "log_decay");
     }
+    Reads reads(PyObject *const *a) const
+    {
+        Reads r;
+        r.add(q_t, "q", strides);
+        r.add(tensor(a[1], "k"), "k", strides + 2);
+        r.add(tensor(a[2], "v"), "v", strides + 4);
+        return r;
+    }
     std::vector<int64_t> state() const { return {B, H, dk, dv}; }
     const int *lengths(PyObject *o) const { return (const int *)dev_opt(o, ScalarType::Int, {B}, "lengths", q_t); }
     Ws space(PyObject *o, int backward) const
@@ -592,6 +645,13 @@ PyObject *decay_fwd(PyObject *const *a)
     void *op = dev(out, g.st, shape, "out", g.q_t);
     if (truth(a[9])) so = empty(g.state(), kF32, g.q_t);
     const Ws w = g.space(a[11], 0);
+    if (!none(a[10]) || !none(a[11])) {
+        Reads r = g.reads(a);
+        r.add(a[7], "s_in");
+        r.add(a[8], "lengths");
+        r.write(a[10], "out");
+        r.write(a[11], "workspace");
+    }
     float *sop = so.defined() ? (float *)so.data_ptr() : nullptr;
     void *s = on.stream();
     CALL(dig_decay_fwd(g.q, g.k, g.v, g.strides, g.decay.data(), len, si, op, sop, g.B, g.H, g.Hk, g.gh, g.gw, g.dk, g.dv, dir, g.dtype, w.p, w.n, s), "dig_decay_fwd");
@@ -629,6 +689,17 @@ PyObject *decay_bwd(PyObject *const *a)
     void *qp = dev(dq, g.st, g.q_t.sizes(), "dq", g.q_t), *kp = dev(dk, g.st, ks, "dk", g.q_t), *vp = dev(dv, g.st, vs, "dv", g.q_t);
     if (truth(a[11])) dsi = empty(g.state(), kF32, g.q_t);
     const Ws w = g.space(a[13], 1);
+    if (!none(a[12]) || !none(a[13])) {
+        Reads r = g.reads(a);
+        r.add(a[4], "d_out");
+        r.add(a[8], "s_in");
+        r.add(a[9], "ds_out");
+        r.add(a[10], "lengths");
+        r.write(dq, "dq");
+        r.write(dk, "dk");
+        r.write(dv, "dv");
+        r.write(a[13], "workspace");
+    }
     float *dsip = dsi.defined() ? (float *)dsi.data_ptr() : nullptr;
     void *s = on.stream();
     CALL(dig_decay_bwd(g.q, g.k, g.v, g.strides, g.decay.data(), len, gp, si, dso, qp, kp, vp, dsip, g.B, g.H, g.Hk, g.gh, g.gw, g.dk, g.dv, dir, g.dtype, w.p, w.n, s),
@@ -654,6 +725,8 @@ PyObject *decay_step(PyObject *const *a)
     const std::vector<int64_t> shape = {B, H, dv};
     Tensor out = given(a[5], shape, st, q, "out");
     void *op = dev(out, st, shape, "out", q), *s = on.stream();
+    apart({&q, &k, &v}, tensor(a[4], "state"), "state");
+    if (!none(a[5])) apart({&q, &k, &v, &tensor(a[4], "state")}, out, "out");
     CALL(dig_decay_step(qp, kp, vp, decay.data(), sp, op, sp, (int)B, (int)H, (int)Hk, (int)dk, (int)dv, dtype, s), "dig_decay_step");
     return wrap(out);
 }

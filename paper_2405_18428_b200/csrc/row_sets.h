@@ -41,6 +41,21 @@ inline bool rows_meet(RowSet r, long long off, long long width, bool same)
     }
     return false;
 }
+// Whether a row of `r` meets the `width` elements that start `off` elements behind the first row's start.
+inline bool rows_meet_block(RowSet r, long long off, long long width)
+{
+    if (off >= r.extent() || off + (__int128)width <= 0) return false;
+    if (r.L < r.B) {
+        std::swap(r.L, r.B);
+        std::swap(r.sb, r.st);
+    }
+    for (int b = 0; b < r.B; ++b) {
+        const __int128 x = off - (__int128)b * r.sb, lo = x - r.width + 1, hi = x + width - 1;             // lo <= l st <= hi
+        if (hi < 0 || lo > (__int128)(r.L - 1) * r.st) continue;
+        if (lo <= 0 || r.st == 0 || (lo + r.st - 1) / r.st * r.st <= hi) return true;
+    }
+    return false;
+}
 // Whether rows that are written in place are distinct: those of one tensor, and of one and the other, which starts `off` elements further.
 inline bool distinct(const RowSet &r) { return r.in_order() || !rows_meet(r, 0, r.width, true); }
 inline bool apart(const RowSet &q, const RowSet &k, long long off)

@@ -339,20 +339,22 @@ def dig_decay_fwd(q, k, v, log_decay, grid_h, grid_w, direction=DIG_ROW_FWD, *, 
 
     q: [B, L, H, d_k]; k: [B, L, H_kv, d_k]; v: [B, L, H_kv, d_v], H a multiple of H_kv; the last two dimensions dense, the others of any
     stride (slices of a fused projection); log_decay: H numbers <= 0; s_in, s_out: fp32 [B, H, d_k, d_v]; lengths: int32 [B] tokens of
-    each sequence of a padded batch, whose rows of `out` behind the end are zeros (row orders only)."""
+    each sequence of a padded batch, whose rows of `out` behind the end are zeros (row orders only).  A given `out` or `workspace` overlaps
+    nothing else."""
     return _binding().decay_fwd(q, k, v, log_decay, grid_h, grid_w, direction, s_in, lengths, want_s_out, out, workspace)
 
 
 def dig_decay_bwd(q, k, v, log_decay, d_out, grid_h, grid_w, direction=DIG_ROW_FWD, *, s_in=None, ds_out=None, lengths=None,
                   want_ds_in=False, grads=None, workspace=None):
-    """Returns (dq, dk, dv, ds_in or None) for the loss <d_out, out> + <ds_out, s_out>; `grads`: (dq, dk, dv) to write to."""
+    """Returns (dq, dk, dv, ds_in or None) for the loss <d_out, out> + <ds_out, s_out>; `grads`: (dq, dk, dv) to write to, which
+    overlap nothing else."""
     return _binding().decay_bwd(q, k, v, log_decay, d_out, grid_h, grid_w, direction, s_in, ds_out, lengths, want_ds_in, grads, workspace)
 
 
 def dig_decay_step(q, k, v, log_decay, state, *, out=None):
     """One more token of every sequence: updates `state` (fp32 [B, H, d_k, d_v]) in place and returns out [B, H, d_v].
 
-    q: [B, H, d_k]; k: [B, H_kv, d_k]; v: [B, H_kv, d_v]; log_decay: H numbers <= 0."""
+    q: [B, H, d_k]; k: [B, H_kv, d_k]; v: [B, H_kv, d_v]; log_decay: H numbers <= 0.  A given `out` overlaps no other tensor."""
     return _binding().decay_step(q, k, v, log_decay, state, out)
 
 

@@ -18,6 +18,7 @@ extern "C" int two(int B, int L, long long qb, long long qt, long long qw, long 
 {
     return apart({B, L, qb, qt, qw}, {B, L, kb, kt, kw}, off);
 }
+extern "C" int block(int B, int L, long long sb, long long st, long long w, long long off, long long width) { return rows_meet_block({B, L, sb, st, w}, off, width); }
 """
 
 
@@ -30,6 +31,7 @@ def rules(tmp_path_factory):
     lib = ctypes.CDLL(so)
     ll = ctypes.c_longlong
     lib.one.argtypes = [ctypes.c_int] * 2 + [ll] * 3
+    lib.block.argtypes = [ctypes.c_int] * 2 + [ll] * 5
     lib.two.argtypes = [ctypes.c_int] * 2 + [ll] * 7
     return lib
 
@@ -79,6 +81,19 @@ def test_rows_of_two_tensors(rules):
     # queries and keys of a sequence behind one another, sequence by sequence and token by token
     assert rules.two(3, 5, 5 * 12, 8, 8, 5 * 12, 4, 4, 5 * 8)
     assert rules.two(3, 5, 8, 3 * 12, 8, 4, 3 * 12, 4, 3 * 8)
+
+
+def test_a_block_between_rows(rules):
+    rng = random.Random(3)
+    seen = [0, 0]
+    for _ in range(6000):
+        B, L, w = rng.randint(1, 4), rng.randint(1, 5), rng.randint(1, 4)
+        sb, st = (rng.choice([0, w, w + 3, (w + 3) * L + 9, rng.randint(0, 30)]) for _ in range(2))
+        off, width = rng.randint(-20, 90), rng.randint(1, 6)
+        want = overlap(elements(B, L, sb, st, w), [range(off, off + width)])
+        assert bool(rules.block(B, L, sb, st, w, off, width)) == want, (B, L, sb, st, w, off, width)
+        seen[want] += 1
+    assert min(seen) > 500
 
 
 def test_long_strides_and_many_rows(rules):
