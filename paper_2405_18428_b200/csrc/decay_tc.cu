@@ -748,16 +748,12 @@ __global__ void __launch_bounds__(LocalCfg<D>::THREADS, 2) decay_local(const __g
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tm = ctl.tmem;
-    // Tiles whose tokens all count with a power of the decay that is 0 in fp32 are left out.
+    // Tokens whose power of the decay is 0 in fp32 count too: 0 times a NaN or an infinity is a NaN, as in the passes.  (Without their tiles 5 x 2500
+    // tokens of 16 heads of 128 channels, slopes, took 98.3 us instead of 99.9.)
     auto next_item = [&](int item, Item &w, int &end) {
         w = item_at(a, item);
         end = min((w.t0 + a.G) * T, w.n);
         if (w.seg == a.nseg - 1 && !a.pass[w.pass].final) w.t_end = w.t0 = w.t1;           // goes into the final state only
-        const float lam = a.lam.v[w.h];
-        if (lam * (float)(end - w.t0 * T) < -130.f) {
-            const int far = end - ((int)(-130.f / lam) + 2) - T;             // tiles up to that of this position
-            if (far >= 0) w.t0 = max(w.t0, far / T + 1);
-        }
     };
     int i = 0, done = 0;                         // tiles and items with any so far
     if (warp == 8 || warp == 9) {
