@@ -1,6 +1,7 @@
 // Rotary positions with several axes.  Pair i of a head's channels is turned by positions[token][axis[i]] * freq[i]; the inverse
-// rotation is the gradient of the rotation.  Angles are formed in 64 bits, in turns, and reduced before they are rounded to fp32: far
-// positions (2^31 at frequency 1) keep angles within 2e-7.
+// rotation is the gradient of the rotation.  Angles are formed in 64 bits, in turns, and reduced before they are rounded to fp32, with what
+// the rounded product leaves and 1 / (2 pi) in two parts: far positions (2^31 at frequency 1) keep angles within 1e-7, the rounding to fp32 (one product with one
+// part of 1 / (2 pi): 3.2e-7).
 // Moved once: q and k in and out.  A token's angles are computed once by its CTA and serve all of its heads.
 #include <cmath>
 
@@ -10,6 +11,8 @@ namespace dig {
 namespace {
 
 constexpr int kMaxPairs = 64, kNT = 256, kMaxTokens = 8, kCtas = 4;          // kCtas: on an SM
+
+constexpr double kTurn = 0x1.45f306dc9c883p-3, kTurnLow = -0x1.6b01ec5417056p-57;            // 1 / (2 pi) and what its rounding leaves
 
 // Division of i < 2^31 through the reciprocal rounded up: the estimate is at most one too large.
 struct Div {
@@ -31,7 +34,7 @@ struct RopeArgs {
     int L, d, n, axes, tokens;       // n: pairs; tokens of a CTA
     Div by_token, by_head;           // units of a token, of a head
     long long total;                 // B * L
-    double turns[kMaxPairs];         // freq / (2 pi), negative for the inverse
+    double freqs[kMaxPairs];         // negative for the inverse
     unsigned char axis[kMaxPairs];
 };
 
@@ -97,13 +100,13 @@ __global__ void __launch_bounds__(kNT, kCtas) rope(const __grid_constant__ RopeA
     using U = typename Vec<T, E>::U;
     // apart, so that lanes read consecutive vectors of them
     __shared__ __align__(16) float cosines[kMaxTokens * kMaxPairs], sines[kMaxTokens * kMaxPairs];
-    __shared__ double turns[kMaxPairs];
+    __shared__ double freqs[kMaxPairs];
     __shared__ int axis[kMaxPairs];
     __shared__ long long xo[2][kMaxTokens], yo[2][kMaxTokens];               // where a token's q and k stand
     const long long first = (long long)blockIdx.x * a.tokens;
     const int here = (int)min((long long)a.tokens, a.total - first), n = a.n;
     if (threadIdx.x < n) {
-        turns[threadIdx.x] = a.turns[threadIdx.x];
+        freqs[threadIdx.x] = a.freqs[threadIdx.x];
         axis[threadIdx.x] = a.axis[threadIdx.x];
     }
     if (threadIdx.x < 2 * here) {
@@ -145,8 +148,9 @@ __global__ void __launch_bounds__(kNT, kCtas) rope(const __grid_constant__ RopeA
     for (int i = threadIdx.x; i < here * n; i += kNT) {
         const int t = i / n, j = i - t * n;
         const uint32_t tok = (uint32_t)(first + t), b = tok / (uint32_t)a.L;
-        const double z = a.pos[b * a.pos_batch + (long long)(tok - b * a.L) * a.axes + axis[j]] * turns[j];
-        sincospif((float)(2.0 * (z - rint(z))), sines + i, cosines + i);
+        const double p = a.pos[b * a.pos_batch + (long long)(tok - b * a.L) * a.axes + axis[j]], f = freqs[j], z = __dmul_rn(p, f), low = fma(p, f, -z);
+        const double turn = fma(low, kTurn, fma(z, kTurnLow, fma(z, kTurn, -rint(z * kTurn))));
+        sincospif((float)(2.0 * turn), sines + i, cosines + i);
     }
     __syncthreads();
     for (uint32_t i0 = threadIdx.x; i0 < count; i0 += kTurns * kNT) {
@@ -226,7 +230,7 @@ dig_status launch_rope(const void *q, const void *k, const long long *strides, c
     a.L = L; a.d = d; a.n = n_pairs; a.axes = n_axes; a.total = (long long)B * L;
     if (a.total > 0x7fffffffll) return DIG_ERR_UNSUPPORTED;
     for (int i = 0; i < n_pairs; ++i) {
-        a.turns[i] = (inverse ? -freqs[i] : freqs[i]) * 0.15915494309189533577;
+        a.freqs[i] = inverse ? -freqs[i] : freqs[i];
         a.axis[i] = (unsigned char)axes[i];
     }
     const bool f = dtype == DIG_F32;
