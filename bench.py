@@ -26,6 +26,7 @@ import hashlib
 import json
 import math
 import os
+import re
 import sys
 import threading
 import time
@@ -114,18 +115,24 @@ def kernel_alg_bytes(wl):
     return out
 
 
-def source_hash():
+def source_hash(name):
+    """Of a kernel's file and of the headers beside it that it includes, directly or through one another."""
+    src, seen, todo = os.path.join(ROOT, "paper_2405_18428_b200", "csrc"), {}, [name]
+    while todo:
+        f = todo.pop()
+        path = os.path.join(src, f)
+        if f not in seen and os.path.exists(path):
+            seen[f] = open(path, "rb").read()
+            todo += re.findall(r'^#include "([^"]+)"', seen[f].decode(), re.M)
     h = hashlib.sha256()
-    src = os.path.join(ROOT, "paper_2405_18428_b200", "csrc")
-    for f in sorted(os.listdir(src)):
-        if f.endswith((".cu", ".cuh")):
-            h.update(open(os.path.join(src, f), "rb").read())
+    for f in sorted(seen):
+        h.update(f.encode() + b"\0" + seen[f])
     return h.hexdigest()[:16]
 
 
 def recorded_traffic(kernel, workload):
     """DRAM bytes per launch of a kernel from the ncu capture recorded beside the profile summaries;
-    None when no capture exists for this kernel and workload or the kernel sources changed since."""
+    None when no capture exists for this kernel and workload or its sources have changed since."""
     path = os.path.join(ROOT, "profiles", "dram_traffic.json")
     if not os.path.exists(path):
         return None
@@ -133,11 +140,9 @@ def recorded_traffic(kernel, workload):
         rec = json.load(open(path))
     except ValueError:
         return None
-    if rec.get("source_hash") != source_hash():
-        return None
     for r in rec.get("kernels", []):
         if r["kernel"].startswith(kernel) and r["workload"] == workload:
-            return r["dram_bytes_per_launch"]
+            return r["dram_bytes_per_launch"] if rec["sources"].get(r["source"]) == source_hash(r["source"]) else None
     return None
 
 
