@@ -272,7 +272,8 @@ dig_status dig_gla_bwd_multi(const void *q, const void *k, const void *v, const 
  * dig_gla_fwd with one constant gate per head (constant decays as of retention layers, 1 - 2^-5 ... , or slopes 2^(-8 h / H)), without
  * the gate tensor's bytes.  Nothing of the paper: DiG's gates depend on the token.  No scaling and no normaliser are applied.
  *   q: [B][L][H][d_k]; k: [B][L][H_kv][d_k]; v: [B][L][H_kv][d_v]; out: [B][L][H][d_v], dense; H a multiple of H_kv, and head h reads
- *   key/value head h / (H / H_kv).  d_k, d_v: multiples of 8, 8..128; H at most 256.  `dtype`: DIG_F32 or DIG_BF16.
+ *   key/value head h / (H / H_kv).  d_k, d_v: multiples of 8, 8..128; H at most 256, B * H at most 65535 (here, in dig_decay_bwd and dig_decay_step).  `dtype`: DIG_F32 or DIG_BF16;
+ *   bf16 results of 2^35 elements or more are refused (DIG_ERR_UNSUPPORTED).
  *   strides: HOST array of the batch and token strides of q, k and v in elements (q batch, q token, k batch, ...), multiples of 16
  *   bytes, or NULL where all three are dense; the heads of a token always stand side by side.  Slices of a fused projection
  *   [B][L][(H + H_kv) d_k + H_kv d_v] need no copy so.
@@ -323,13 +324,13 @@ dig_status dig_rope(const void *q, const void *k, const long long *strides, cons
 
 /* Layer norm over rows of D values, the norm in front of a mixer block:
  *   y = (x - mean) / sqrt(var + eps) * w + b,   biased variance.
- *   x, y: [rows][D]; w, b: fp32 [groups][D] or NULL (1 / 0), group i serving rows i * rows / groups ... (an image's scale and shift,
+ *   x, y: [rows][D], which do not overlap; w, b: fp32 [groups][D] or NULL (1 / 0), group i serving rows i * rows / groups ... (an image's scale and shift,
  *   groups = 1: one set for all); rows a multiple of groups; D in 1..8192; groups at most 65535.  `dtype`: DIG_F32 or DIG_BF16. */
 dig_status dig_layernorm_fwd(const void *x, const float *w, const float *b, void *y, long long rows, int groups, int D, float eps, int dtype,
                              void *cuda_stream);
 
 /* Reverse mode of dig_layernorm_fwd: dx from dy, and where the pointer is not NULL dw and db (fp32 [groups][D]; the gradients at weight 1
- * where w is NULL), summed over a group's rows in a fixed order.  The workspace (dig_layernorm_bwd_workspace_bytes; 0 for invalid sizes)
+ * where w is NULL), summed over a group's rows in fp32 in a fixed order.  Results overlap no input.  The workspace (dig_layernorm_bwd_workspace_bytes; 0 for invalid sizes)
  * holds partial sums and is needed only when dw or db is requested. */
 size_t dig_layernorm_bwd_workspace_bytes(long long rows, int groups, int D);
 dig_status dig_layernorm_bwd(const void *x, const void *dy, const float *w, void *dx, float *dw, float *db, long long rows, int groups, int D,

@@ -17,8 +17,9 @@
 //   warps 20 .. 22  loads of q, k, v;  warp 23  products
 // Five parts on every scheduler share its instruction cache: loops are kept short and rolled, and what is rare stands apart.  Unrolled, two
 // thirds of the warps' time went by waiting for instructions (4 x 4096 tokens of 12 heads of 64 channels: 60 us, 30 rolled).
-// A tile of 64 channels takes 3700 cycles, 17 bytes a cycle and SM in and out: two thirds of the copy bandwidth; issue slots are 60 % busy.  The
-// loads are issued by single warps, a tile of rows in 2600 cycles; free of charge they would make it 3430.
+// A tile of 64 channels takes 3700 cycles, 17 bytes a cycle and SM in and out: two thirds of the copy bandwidth; issue slots are 60 % busy, warps
+// that poll barriers included.  The loads are issued by single warps, a tile of rows in 2600 cycles; with all rows at one address, which spares their time in
+// memory but not their instructions, a tile takes 3430.  The widest heads spill (120 bytes a thread stored, at 80 registers).
 #include <type_traits>
 
 #include "decay_plan.cuh"

@@ -91,7 +91,7 @@ __device__ __forceinline__ void angles(const float *p, float (&f)[V])
 
 // V pairs per thread and turn: neighbours (2 i, 2 i + 1) where INTER, else (i, i + n).  kTurns turns' loads are on their way together, the first
 // ones while the angles are formed (with the angles first: 48 us for 16384 tokens of 32 heads of 72; 34 so, 4.4 TB/s, where a plain copy of as
-// many bytes takes 27).
+// many bytes takes 27).  The widest accesses (eight pairs in bf16, four in fp32, by halves) spill 40 bytes at the 64 registers that four CTAs leave.
 constexpr int kTurns = 4;
 template <typename T, int V, bool INTER>
 __global__ void __launch_bounds__(kNT, kCtas) rope(const __grid_constant__ RopeArgs a)
