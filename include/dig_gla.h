@@ -285,7 +285,7 @@ dig_status dig_gla_bwd_multi(const void *q, const void *k, const void *v, const 
  * Results overlap no input and no other result (here, in dig_decay_bwd and in dig_decay_step, but for its state in place).
  * fp32 storage: fp32 FMA arithmetic.  bf16 storage: q, k and v enter the products as they are, decayed scores, states and (for out) decayed
  * keys as bf16, sums in fp32; s_out is summed apart with decayed keys of 24 bits and has fp32 accuracy.
- * A NaN or an infinity in k or v stays: it makes NaNs of its channels in every later row and in s_out, however far the decay has gone, and one in v
+ * A NaN or an infinity in k or v stays: its channels of every later row and of s_out are NaN or infinite, however far the decay has gone, and one in v
  * reaches rows of the same 32 positions before it (bf16 storage; products with zeros), never earlier ones. */
 size_t dig_decay_workspace_bytes(int B, int H, int H_kv, int grid_h, int grid_w, int d_k, int d_v, int dtype, int backward);
 dig_status dig_decay_fwd(const void *q, const void *k, const void *v, const long long *strides, const float *log_decay_per_head,
